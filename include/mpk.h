@@ -537,6 +537,99 @@ mpk_status mpk_serve_state(mpk_server *s, int32_t *buf, size_t cap, size_t *need
 const float *mpk_serve_logits(const mpk_server *s);
 void mpk_serve_destroy(mpk_server *s);
 
+/* ----------------------------------------------------------------------------------------------
+ * Rows beside the decode step: many rows of a layer at once, on the cache of a compiled graph, and
+ * what rows of logits say about tokens.  A decode step appends one K/V row a sequence and attends
+ * with one query row; these calls do the same for any number of rows of up to `batch` sequences, so
+ * that a program which runs the projections of a prompt itself fills the cache its graph then
+ * decodes from, layer by layer: projections, mpk_rows_append, mpk_rows_attend, the rest of the layer.
+ *
+ * Common to the three
+ *   - the graph says which model, cache, page table and GPU; it is not host_only, not a serving graph
+ *     (its slots and pages belong to its server) and lives on the current device.  Whole models and
+ *     one graph of a set work alike (a set's graph sees the first `batch` slots).
+ *   - asynchronous on `stream`; no allocation, no host synchronisation; may be captured into a HIP
+ *     graph (all lengths are read from device memory when the work runs, so a replay follows them).
+ *   - calls on one graph, decode steps included, must not overlap in time where one of them writes
+ *     what the other reads or writes: cache rows, outputs, workspaces.
+ *   - what only the device can see (a row list that does not ascend, a position, slot, page or token
+ *     out of range) is reported by mpk_graph_status as MPK_ERR_DEVICE, never dereferenced; the
+ *     sequence or row concerned is left out (details below).  The error word keeps the first error
+ *     until mpk_graph_reset.
+ *   - results do not depend on timing: the same call gives the same bits.
+ * -------------------------------------------------------------------------------------------- */
+typedef enum { MPK_ROWS_BF16 = 0, MPK_ROWS_F32 = 1 } mpk_rows_type;
+
+/* Device memory that mpk_rows_attend and mpk_rows_logprobs work in, given by the caller (16-byte
+ * aligned, contents of no matter before and after).  Calls that may overlap in time, replays of captured
+ * ones among them, need one each. */
+#define MPK_ROWS_WORKSPACE_BYTES (96u << 20)
+
+/* Query/key norm (MPK_MODEL_QK_NORM), position rotation, append to the KV cache.
+ *   layer     : the layer whose cache rows are written and whose q_norm / k_norm are used
+ *   n_seqs    : sequences of this call, 1 .. batch
+ *   n_rows    : rows that qkv and q_out have (0: nothing to do)
+ *   row_begin : device int32 [n_seqs + 1], ascending, within 0 .. n_rows: sequence i has rows
+ *               row_begin[i] .. row_begin[i + 1] - 1 (possibly none).  Rows before the first and
+ *               behind the last sequence are neither read nor written
+ *   slots     : device int32 [n_seqs], the cache slot (batch row) of each sequence, no slot twice among
+ *               sequences that have rows; NULL: sequence i has slot i
+ *   positions : device int32 [n_seqs]: rows already cached; the sequence's rows get the positions
+ *               positions[i], positions[i] + 1, .., all below max_seq
+ *   qkv       : device [n_rows][row stride qkv_stride elements], bf16 or fp32 (qkv_type): the outputs
+ *               of the fused QKV projection, (n_q_heads + 2 n_kv_heads) head_dim a row.  16-byte
+ *               aligned, strides multiples of 8 elements
+ *   q_out     : device bf16 [n_rows][row stride q_stride elements], n_q_heads head_dim a row: the
+ *               queries, normed and rotated.  May be qkv itself with the same stride (bf16): the
+ *               queries are then rotated in place
+ * K and V rows are written to the cache as a decode step writes them: fp32 arithmetic, angles in fp64,
+ * rounded to bf16 once.  A paged cache's rows go to the pages the table names for them.
+ * Device errors: row_begin not ascending or outside 0 .. n_rows (nothing is written); a slot outside
+ * 0 .. batch - 1 or used by an earlier sequence, a position below 0 or at or above max_seq (the
+ * sequence is left out); a page outside the pool (its rows of K and V are left out). */
+mpk_status mpk_rows_append(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows,
+                           const int32_t *row_begin, const int32_t *slots, const int32_t *positions,
+                           const void *qkv, uint32_t qkv_type, size_t qkv_stride, void *q_out,
+                           size_t q_stride, void *stream);
+
+/* Attention of rows over the cache: the row at position p of a sequence attends to the sequence's
+ * cache rows 0 .. p (its own among them: append first), scores / sqrt(head_dim), softmax.
+ *   layer .. positions : as above
+ *   q   : device bf16 [n_rows][row stride q_stride], n_q_heads head_dim a row, as mpk_rows_append leaves
+ *         them (q_out, or qkv rotated in place)
+ *   out : device bf16 [n_rows][row stride out_stride], n_q_heads head_dim a row; not q.  16-byte aligned,
+ *         strides multiples of 8 elements
+ *   workspace : device, MPK_ROWS_WORKSPACE_BYTES
+ * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the product with
+ * V, the output once at the end.  Cache rows above a row's position never reach it, whatever they hold
+ * (NaN and infinities included).
+ * Device errors as above; with a page outside the pool the sequence's outputs are undefined. */
+mpk_status mpk_rows_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows,
+                           const int32_t *row_begin, const int32_t *slots, const int32_t *positions,
+                           const void *q, size_t q_stride, void *out, size_t out_stride,
+                           void *workspace, void *stream);
+
+/* What rows of logits say: with p = softmax(row) over the graph's vocab,
+ *   logits       : device [n_rows][row stride row_stride elements], bf16 or fp32 (logits_type): what a
+ *                  decode step writes, logits_all of mpk_decode_steps, an LM head over prompt rows.  Any
+ *                  alignment of the element type, any stride >= vocab; n_rows 0: nothing to do
+ *   tokens       : device int32 [n_rows]: the token asked about, -1: none (its logprob is 0)
+ *   logprobs     : device fp32 [n_rows]: ln p[token]   (tokens and logprobs: both or neither NULL)
+ *   entropy      : device fp32 [n_rows] or NULL: -sum p ln p, in nats
+ *   n_top        : alternatives a row, 0 .. min(32, vocab)
+ *   top_tokens   : device int32 [n_rows][n_top]: the most probable tokens, of equal logits the lower
+ *                  index first (both NULL if n_top is 0)
+ *   top_logprobs : device fp32 [n_rows][n_top]: their ln p
+ *   workspace    : device, MPK_ROWS_WORKSPACE_BYTES
+ * A logit of -inf is a token ruled out: ln p = -inf, nothing for the entropy.  A row that holds a NaN or
+ * +inf, or nothing above -inf, has no distribution: logprob (of a token asked about), entropy and
+ * top_logprobs are NaN, top_tokens -1.  Device error: a token outside -1 .. vocab - 1 (its logprob is NaN). */
+#define MPK_ROWS_MAX_TOP 32u
+mpk_status mpk_rows_logprobs(mpk_graph *g, uint32_t n_rows, const void *logits, uint32_t logits_type,
+                             size_t row_stride, const int32_t *tokens, float *logprobs, float *entropy,
+                             uint32_t n_top, int32_t *top_tokens, float *top_logprobs, void *workspace,
+                             void *stream);
+
 const char *mpk_last_error(void);
 void mpk_graph_destroy(mpk_graph *g);
 

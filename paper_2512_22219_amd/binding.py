@@ -106,7 +106,10 @@ SYMBOLS = ("mpk_compile", "mpk_compile_dag", "mpk_decode_step", "mpk_decode_step
            "mpk_set_destroy", "mpk_last_error", "mpk_graph_destroy", "mpk_static_scratch_need",
            "mpk_graph_set_page_table", "mpk_serve_create", "mpk_serve_submit", "mpk_serve_run",
            "mpk_serve_result", "mpk_serve_state", "mpk_serve_logits", "mpk_serve_destroy",
-           "mpk_serve_create_set", "mpk_serve_last_batch", "mpk_serve_status", "mpk_graph_task_forms")
+           "mpk_serve_create_set", "mpk_serve_last_batch", "mpk_serve_status", "mpk_graph_task_forms",
+           "mpk_rows_append", "mpk_rows_attend", "mpk_rows_logprobs")
+ROWS_BF16, ROWS_F32 = 0, 1
+ROWS_MAX_TOP, ROWS_WORKSPACE_BYTES = 32, 96 << 20
 DEBUG_TRACE, DEBUG_POISON, DEBUG_JITTER, DEBUG_LOSE_NOTIFY = 1, 2, 4, 8
 
 _lib = None
@@ -169,8 +172,12 @@ def lib():
         L.mpk_serve_last_batch.restype = C.c_uint32
         L.mpk_serve_status.argtypes = [vp]
         L.mpk_serve_status.restype = C.c_int
-        for n in SYMBOLS[:14] + ("mpk_graph_set_page_table", "mpk_serve_create", "mpk_serve_submit",
-                                 "mpk_serve_run", "mpk_serve_result", "mpk_serve_state"):
+        seqs = [vp] + [C.c_uint32] * 3 + [vp] * 3
+        L.mpk_rows_append.argtypes = seqs + [vp, C.c_uint32, C.c_size_t, vp, C.c_size_t, vp]
+        L.mpk_rows_attend.argtypes = seqs + [vp, C.c_size_t, vp, C.c_size_t, vp, vp]
+        L.mpk_rows_logprobs.argtypes = [vp, C.c_uint32, vp, C.c_uint32, C.c_size_t, vp, vp, vp, C.c_uint32, vp, vp, vp, vp]
+        for n in SYMBOLS[:14] + ("mpk_rows_append", "mpk_rows_attend", "mpk_rows_logprobs",
+                                 "mpk_graph_set_page_table", "mpk_serve_create", "mpk_serve_submit", "mpk_serve_run", "mpk_serve_result", "mpk_serve_state"):
             getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -263,6 +270,27 @@ class Graph:
 
     def set_page_table(self, page_table_ptr: int):
         _check(lib().mpk_graph_set_page_table(self._h, page_table_ptr))
+
+    def rows_append(self, layer: int, n_seqs: int, n_rows: int, row_begin_ptr: int, slots_ptr: int, positions_ptr: int, qkv_ptr: int,
+                    qkv_type: int, qkv_stride: int, q_out_ptr: int, q_stride: int, stream: int = 0):
+        """Norm, rotate and append rows of up to `batch` sequences to the cache (strides in elements; slots_ptr 0: sequence i
+        has slot i; qkv_type ROWS_BF16 or ROWS_F32)."""
+        _check(lib().mpk_rows_append(self._h, layer, n_seqs, n_rows, row_begin_ptr, slots_ptr or None, positions_ptr, qkv_ptr,
+                                     qkv_type, qkv_stride, q_out_ptr, q_stride, stream))
+
+    def rows_attend(self, layer: int, n_seqs: int, n_rows: int, row_begin_ptr: int, slots_ptr: int, positions_ptr: int, q_ptr: int,
+                    q_stride: int, out_ptr: int, out_stride: int, workspace_ptr: int, stream: int = 0):
+        """Attention of those rows over the cache; workspace: ROWS_WORKSPACE_BYTES of device memory."""
+        _check(lib().mpk_rows_attend(self._h, layer, n_seqs, n_rows, row_begin_ptr, slots_ptr or None, positions_ptr, q_ptr,
+                                     q_stride, out_ptr, out_stride, workspace_ptr, stream))
+
+    def rows_logprobs(self, n_rows: int, logits_ptr: int, logits_type: int, row_stride: int, tokens_ptr: int, n_top: int,
+                      logprobs_ptr: int, entropy_ptr: int, top_tokens_ptr: int, top_logprobs_ptr: int, workspace_ptr: int,
+                      stream: int = 0):
+        """Log probability of a token, entropy and n_top alternatives of rows of logits; what is not wanted is 0."""
+        _check(lib().mpk_rows_logprobs(self._h, n_rows, logits_ptr, logits_type, row_stride, tokens_ptr or None, logprobs_ptr or None,
+                                       entropy_ptr or None, n_top, top_tokens_ptr or None, top_logprobs_ptr or None, workspace_ptr,
+                                       stream))
 
     def serve(self, max_requests: int, max_prompt: int, max_new: int, eos_token: int = -1) -> "Server":
         cfg = ServeConfig(C.sizeof(ServeConfig), max_requests, max_prompt, max_new, eos_token)

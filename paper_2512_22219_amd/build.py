@@ -12,8 +12,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 _OBJ = os.path.join(_HERE, "_build")
 LIB = os.path.join(_HERE, "libmpk.so")
-SOURCES = [os.path.join(_CSRC, f) for f in ("compiler.cpp", "runtime.hip", "variants.hip")]
-HEADERS = [os.path.join(_CSRC, "mpk_internal.h"), os.path.join(_CSRC, "kernels.h"),
+SOURCES = [os.path.join(_CSRC, f) for f in ("compiler.cpp", "runtime.hip", "variants.hip", "rows.hip")]
+HEADERS = [os.path.join(_CSRC, "mpk_internal.h"), os.path.join(_CSRC, "kernels.h"), os.path.join(_CSRC, "rows.h"),
            os.path.join(os.path.dirname(_HERE), "include", "mpk.h")]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-I" + os.path.join(os.path.dirname(_HERE), "include"),
@@ -68,7 +68,8 @@ def build(force: bool = True, jobs: int = 8) -> str:
         return LIB
     os.makedirs(_OBJ, exist_ok=True)
     work = [(SOURCES[0], os.path.join(_OBJ, "compiler.o"), [], None),
-            (SOURCES[1], os.path.join(_OBJ, "runtime.o"), [], None)]
+            (SOURCES[1], os.path.join(_OBJ, "runtime.o"), [], None),
+            (SOURCES[3], os.path.join(_OBJ, "rows.o"), [], None)]
     work += [(SOURCES[2], os.path.join(_OBJ, f"variant{v['index']}.o"), [f"-DMPK_VARIANT_INDEX={v['index']}", v["level"], _USAGE], v)
              for v in variants()]
     # the matrix-core sets with experts take longest: start them first

@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "rows.h"
 
 namespace mpk {
 
@@ -129,6 +130,9 @@ struct mpk_graph {
   void* launch_out[2] = {nullptr, nullptr};   // host copy of GraphConst::tokens_out / logits_all (source of the async copy)
   const int32_t* page_table = nullptr;        // paged cache: the table the attention tasks read (device)
   struct mpk_server* server = nullptr;        // serving graph: the server attached to it
+  // what the calls on rows (mpk_rows_*) need of the model
+  uint16_t *cache_k = nullptr, *cache_v = nullptr;
+  std::vector<std::pair<const uint16_t*, const uint16_t*>> qk_gains;   // per layer: q_norm, k_norm (null without the norm)
 };
 
 #define HIP_TRY(expr)                                                              \
@@ -512,6 +516,11 @@ extern "C" mpk_status mpk_compile(const mpk_model_config* cfg, const mpk_weight_
       if ((st = upload(&g->d_const_static, csv)) != MPK_OK) return fail(st);
     }
   }
+  g->cache_k = (uint16_t*)kv->k;
+  g->cache_v = (uint16_t*)kv->v;
+  const bool qk_norm = (cfg->flags & MPK_MODEL_QK_NORM) != 0;
+  for (uint32_t l = 0; l < cfg->n_layers; ++l)
+    g->qk_gains.emplace_back(qk_norm ? (const uint16_t*)weights->layers[l].q_norm : nullptr, qk_norm ? (const uint16_t*)weights->layers[l].k_norm : nullptr);
   *out = g;
   return MPK_OK;
 }
@@ -691,6 +700,12 @@ extern "C" mpk_status mpk_graph_status(mpk_graph* g) {
       return MPK_ERR_DEVICE;
     case DE_BAD_META:
       set_error("an expert task found an inconsistent meta-tensor (expert %u, %u tokens)", err[2], err[3]);
+      return MPK_ERR_DEVICE;
+    case DE_BAD_ROWS:
+      set_error("row_begin does not ascend within the call's rows: sequence %u ends at %d", err[2], (int)err[3]);
+      return MPK_ERR_DEVICE;
+    case DE_BAD_SLOT:
+      set_error("sequence %u has slot %d, outside [0, batch) or an earlier sequence's", err[2], (int)err[3]);
       return MPK_ERR_DEVICE;
     default: set_error("unknown device error %u", err[0]); return MPK_ERR_DEVICE;
   }
@@ -1093,6 +1108,127 @@ extern "C" void mpk_serve_destroy(mpk_server* s) {
   }
   server_free(s);
   delete s;
+}
+
+// ------------------------------------------------------------------ rows beside the decode step
+// Arguments are looked at first, whether the graph can run anything last: what a call refuses can be tried without a GPU.
+static mpk_status rows_runnable(const mpk_graph* g) {
+  if (g->h.opt.serving) { set_error("a serving graph's slots and pages belong to its server"); return MPK_ERR_INVALID_ARG; }
+  if (g->host_only) { set_error("graph was compiled host_only"); return MPK_ERR_INVALID_ARG; }
+  int cur = -1;
+  HIP_TRY(hipGetDevice(&cur));
+  if (cur != g->device) { set_error("the graph lives on device %d, device %d is current", g->device, cur); return MPK_ERR_INVALID_ARG; }
+  return MPK_OK;
+}
+static mpk_status rows_buffer(const char* name, const void* p, size_t stride, size_t least) {
+  if (!p || (uintptr_t)p % 16) { set_error("%s is NULL or not 16-byte aligned", name); return MPK_ERR_INVALID_ARG; }
+  if (stride < least || stride % 8) { set_error("%s: a row stride of %zu elements, expected a multiple of 8 of at least %zu", name, stride, least); return MPK_ERR_INVALID_ARG; }
+  return MPK_OK;
+}
+static mpk_status rows_work(const void* workspace) {
+  if (!workspace || (uintptr_t)workspace % 16) { set_error("workspace is NULL or not 16-byte aligned"); return MPK_ERR_INVALID_ARG; }
+  return MPK_OK;
+}
+constexpr uint32_t kRowsMost = 1u << 24;   // rows of a call
+static mpk_status rows_count(uint32_t n_rows) {
+  if (n_rows > kRowsMost) { set_error("n_rows %u is above %u", n_rows, kRowsMost); return MPK_ERR_INVALID_ARG; }
+  return MPK_OK;
+}
+static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
+                            const int32_t* slots, const int32_t* positions, RowSeqs* s) {
+  if (!g || !row_begin || !positions) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  const HostGraph& h = g->h;
+  if (h.cfg.batch == 0) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
+  if (layer >= h.cfg.n_layers) { set_error("layer %u, the model has %u", layer, h.cfg.n_layers); return MPK_ERR_INVALID_ARG; }
+  if (n_seqs == 0 || n_seqs > std::min(h.cfg.batch, kMaxRowSeqs)) { set_error("n_seqs %u is outside 1..%u, the graph's batch", n_seqs, h.cfg.batch); return MPK_ERR_INVALID_ARG; }
+  const mpk_status st = rows_count(n_rows);
+  if (st != MPK_OK) return st;
+  *s = RowSeqs{};
+  s->row_begin = row_begin; s->slots = slots; s->positions = positions;
+  s->n_seqs = n_seqs; s->n_rows = n_rows;
+  s->n_q = h.cfg.n_q_heads; s->n_kv = h.cfg.n_kv_heads; s->head_dim = h.cfg.head_dim;
+  s->batch = h.cfg.batch; s->max_seq = h.cfg.max_seq;
+  s->err = g->d_err;
+  size_t rows = (size_t)(h.opt.kv_batch ? h.opt.kv_batch : h.cfg.batch) * h.cfg.max_seq;   // of one layer and KV head
+  if (h.opt.kv_page_size) {
+    s->table = g->page_table;
+    s->n_pages = h.opt.kv_pages;
+    s->blocks = h.cfg.max_seq / h.opt.kv_page_size;
+    while ((1u << s->page_shift) < h.opt.kv_page_size) ++s->page_shift;
+    rows = (size_t)h.opt.kv_pages * h.opt.kv_page_size;
+  }
+  const size_t at = (size_t)layer * rows * s->n_kv * s->head_dim;
+  if (g->cache_k) { s->k = g->cache_k + at; s->v = g->cache_v + at; }
+  return MPK_OK;
+}
+static mpk_status rows_cache_runnable(const mpk_graph* g) {
+  const mpk_status st = rows_runnable(g);
+  if (st == MPK_OK && g->h.opt.kv_page_size && !g->page_table) { set_error("the graph reads a paged KV cache: give it a page table first (mpk_graph_set_page_table)"); return MPK_ERR_INVALID_ARG; }
+  return st;
+}
+
+extern "C" mpk_status mpk_rows_append(mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
+                                      const int32_t* slots, const int32_t* positions, const void* qkv, uint32_t qkv_type,
+                                      size_t qkv_stride, void* q_out, size_t q_stride, void* stream) {
+  AppendArgs a{};
+  mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
+  if (st != MPK_OK) return st;
+  if (qkv_type > MPK_ROWS_F32) { set_error("unknown qkv_type %u", qkv_type); return MPK_ERR_INVALID_ARG; }
+  const size_t q = (size_t)a.s.n_q * a.s.head_dim;
+  if ((st = rows_buffer("qkv", qkv, qkv_stride, q + 2 * (size_t)a.s.n_kv * a.s.head_dim)) != MPK_OK) return st;
+  if ((st = rows_buffer("q_out", q_out, q_stride, q)) != MPK_OK) return st;
+  if (qkv == q_out && (qkv_type != MPK_ROWS_BF16 || qkv_stride != q_stride)) { set_error("queries are rotated in place in bf16 rows of one stride only"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_cache_runnable(g)) != MPK_OK || !n_rows) return st;
+  a.qkv = qkv; a.qkv_stride = qkv_stride;
+  a.q_out = (uint16_t*)q_out; a.q_stride = q_stride;
+  a.q_norm = g->qk_gains[layer].first; a.k_norm = g->qk_gains[layer].second;
+  a.inv_freq = g->d_inv_freq; a.eps = g->h.cfg.rms_eps;
+  HIP_TRY(launch_rows_append(a, qkv_type == MPK_ROWS_F32, (hipStream_t)stream));
+  return MPK_OK;
+}
+
+extern "C" mpk_status mpk_rows_attend(mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
+                                      const int32_t* slots, const int32_t* positions, const void* q, size_t q_stride, void* out,
+                                      size_t out_stride, void* workspace, void* stream) {
+  AttendArgs a{};
+  mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
+  if (st != MPK_OK) return st;
+  const size_t width = (size_t)a.s.n_q * a.s.head_dim;
+  if ((st = rows_buffer("q", q, q_stride, width)) != MPK_OK) return st;
+  if ((st = rows_buffer("out", out, out_stride, width)) != MPK_OK) return st;
+  if (q == out) { set_error("out is q"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_work(workspace)) != MPK_OK) return st;
+  if ((st = rows_cache_runnable(g)) != MPK_OK || !n_rows) return st;
+  a.q = (const uint16_t*)q; a.q_stride = q_stride;
+  a.out = (uint16_t*)out; a.out_stride = out_stride;
+  a.work = workspace;
+  HIP_TRY(launch_rows_attend(a, (hipStream_t)stream));
+  return MPK_OK;
+}
+
+extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const void* logits, uint32_t logits_type, size_t row_stride,
+                                        const int32_t* tokens, float* logprobs, float* entropy, uint32_t n_top, int32_t* top_tokens,
+                                        float* top_logprobs, void* workspace, void* stream) {
+  if (!g) { set_error("NULL graph"); return MPK_ERR_INVALID_ARG; }
+  const uint32_t vocab = g->h.cfg.vocab;
+  if (!vocab) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
+  if (logits_type > MPK_ROWS_F32) { set_error("unknown logits_type %u", logits_type); return MPK_ERR_INVALID_ARG; }
+  if (!logits || (uintptr_t)logits % (logits_type == MPK_ROWS_F32 ? 4 : 2)) { set_error("logits is NULL or not aligned to its elements"); return MPK_ERR_INVALID_ARG; }
+  if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
+  if (!tokens != !logprobs) { set_error("tokens and logprobs: both or neither"); return MPK_ERR_INVALID_ARG; }
+  if (n_top > std::min(MPK_ROWS_MAX_TOP, vocab)) { set_error("n_top %u is above %u", n_top, std::min(MPK_ROWS_MAX_TOP, vocab)); return MPK_ERR_INVALID_ARG; }
+  if (n_top && (!top_tokens || !top_logprobs)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  mpk_status st = rows_count(n_rows);
+  if (st != MPK_OK || (st = rows_work(workspace)) != MPK_OK) return st;
+  if ((st = rows_runnable(g)) != MPK_OK || !n_rows || (!tokens && !entropy && !n_top)) return st;
+  LogprobArgs a{};
+  a.logits = logits; a.stride = row_stride;
+  a.tokens = tokens; a.logprobs = logprobs; a.entropy = entropy;
+  a.top_tokens = top_tokens; a.top_logprobs = top_logprobs;
+  a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
+  a.work = workspace; a.err = g->d_err;
+  HIP_TRY(launch_rows_logprobs(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
+  return MPK_OK;
 }
 
 extern "C" const char* mpk_last_error(void) { return mpk::last_error(); }
