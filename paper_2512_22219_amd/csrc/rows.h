@@ -52,6 +52,8 @@ struct LogprobArgs {
   uint32_t* err;
 };
 
+// Once per device, before any of the others: what the kernels need beyond the defaults.
+hipError_t rows_prepare();
 // Each checks nothing (the entry points have) and launches on `stream`.
 hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream);

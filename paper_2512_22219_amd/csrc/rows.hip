@@ -182,63 +182,360 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------------------------ attend
-// One wavefront per row and query head: 64 keys at a time, a lane a key for the scores, a lane D / 64 columns for the product.
+// Queries of one KV head are rows of one product: row r of a sequence's T x grp is query head r % grp of token r / grp, so a
+// tile of 128 rows reads each key once for all heads of the group.  A workgroup takes a tile and a run of blocks of 64 keys
+// (a unit); its four wavefronts have 32 rows each.
+//   S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane then holds 16 keys of ONE row (lane & 31), so maximum, exponentials and
+//   sum need one exchange between the two halves of the wavefront, and the probabilities, rounded to bf16, already are the
+//   other operand of O^T = V^T P^T if the keys of a step are counted 8 (j / 4) + 4 half + j % 4.  V^T comes out of the row-major
+//   tile by ds_read_b64_tr_b16.
+// K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
+// (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
+constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
+constexpr uint32_t kAttendMinBlocks = 2;
+constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t lds_u32 __attribute__((address_space(3)));
+
+// How a call's work is cut: every wavefront of both kernels works it out for itself from the lanes' sequences.
+struct Deal {
+  uint32_t tiles, chunks, blocks;   // of the lane's sequence: row tiles, runs of blocks a tile is cut into, blocks of a run
+  uint32_t first_unit;              // units of the sequences with more blocks, which come first
+  uint32_t part;                    // floats of the workspace in front of the sequence's partial results
+  uint32_t total;                   // units of all
+};
 template <int D>
-__global__ void __launch_bounds__(64) rows_attend_kernel(AttendArgs a) {
-  __shared__ float qs[D], ps[64];
-  __shared__ uint64_t vat[64];
+__device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, uint32_t lg) {
+  const uint32_t lane = threadIdx.x & 63u, T = (uint32_t)(q.end - q.begin), rows = T << lg;
+  Deal d;
+  d.tiles = (rows + kTileRows - 1u) / kTileRows;
+  const uint32_t nb = T ? ((uint32_t)q.pos + T + kBlockKeys - 1u) / kBlockKeys : 0u;
+  uint64_t work = 0;
+  for (uint32_t i = 0; i < s.n_seqs; ++i)
+    work += (uint64_t)__builtin_amdgcn_readlane(d.tiles, i) *
+            (((uint32_t)__builtin_amdgcn_readlane(q.pos, i) + (uint32_t)__builtin_amdgcn_readlane(T, i) / 2u) / kBlockKeys + 1u);
+  uint32_t c = (uint32_t)max((uint64_t)kAttendMinBlocks, (work * s.n_kv + kAttendSlots - 1u) / kAttendSlots);
+  for (;; c *= 2u) {   // (long enough that the partial results fit the workspace)
+    d.chunks = nb > c ? (nb + c - 1u) / c : 1u;
+    const float need = d.chunks > 1u ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(min(rows, kTileRows) * (D + 2u)) : 0.f;
+    float sum = 0.f;
+    for (uint32_t i = 0; i < s.n_seqs; ++i) sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(need), i));
+    if (sum <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u)) break;
+  }
+  d.blocks = (nb + d.chunks - 1u) / d.chunks;
+  if (!T) d.chunks = 0;
+  const uint32_t units = d.tiles * d.chunks * s.n_kv, floats = d.chunks > 1u ? units * min(rows, kTileRows) * (D + 2u) : 0u;
+  d.first_unit = d.part = d.total = 0;
+  for (uint32_t i = 0; i < s.n_seqs; ++i) {
+    const uint32_t onb = __builtin_amdgcn_readlane(nb, i), ou = __builtin_amdgcn_readlane(units, i), of = __builtin_amdgcn_readlane(floats, i);
+    if (onb > nb || (onb == nb && i < lane)) d.first_unit += ou;
+    if (i < lane) d.part += of;
+    d.total += ou;
+  }
+  return d;
+}
+// Blocks of keys that the rows of a tile see.
+__device__ __forceinline__ uint32_t tile_blocks(uint32_t pos, uint32_t T, uint32_t tile, uint32_t lg) {
+  const uint32_t t = min(T - 1u, (tile * kTileRows + kTileRows - 1u) >> lg);
+  return (pos + t) / kBlockKeys + 1u;
+}
+
+template <int D>
+__device__ __forceinline__ uint32_t swizzle(uint32_t row) {   // 16-byte piece c of a row of the tile lies at place c ^ swizzle(row)
+  return D == 128 ? ((row & 3u) << 2) | ((row >> 2) & 3u) : (((row >> 1) & 1u) << 2) | ((row >> 2) & 3u);
+}
+
+// 1 KB of the wavefront's lanes' 16 bytes each into LDS at `to` (lane after lane).  Assembly text, for the compiler waits for a
+// load into LDS before any later read of LDS that it cannot tell apart; who issues it waits (drain_vmem).
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
+  const uint64_t p = (uint64_t)base;
+  const u32x4 rsrc = {uniform_u32((uint32_t)p), uniform_u32((uint32_t)(p >> 32) & 0xFFFFu), 0x7FFFFFFFu, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
+}
+
+__device__ __forceinline__ uint32_t nonfinite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }   // bit 15 / 31: lower / upper
+
+template <int D, bool PAGED>
+__global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) {
+  constexpr uint32_t KS = D / 16, NT = D / 32, CPR = D / 8, RPI = 64 / CPR, IPW = 16 / RPI, ROWB = D * 2, TILE = kBlockKeys * ROWB;
+  extern __shared__ __align__(16) unsigned char tiles_lds[];   // K, V of the even blocks, K, V of the odd ones, a flag
+  uint32_t& any_bad = *(uint32_t*)(tiles_lds + 4u * TILE);
   const RowSeqs& s = a.s;
-  const uint32_t lane = threadIdx.x, row = blockIdx.x / s.n_q, h = blockIdx.x - row * s.n_q;
-  const SeqLanes q = load_seqs(s, blockIdx.x == 0);
-  const uint32_t seq = seq_of_row(q, row);
-  if (seq == 64u) return;
-  const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane(q.pos, seq) + row - (uint32_t)__builtin_amdgcn_readlane(q.begin, seq);
-  const uint32_t slot = (uint32_t)__builtin_amdgcn_readlane(q.slot, seq), kvh = h / (s.n_q / s.n_kv);
-  for (uint32_t i = lane; i < D; i += 64) qs[i] = bf16_to_f32(as_global(a.q)[(size_t)row * a.q_stride + (size_t)h * D + i]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o[D / 64] = {};
-  for (uint32_t j0 = 0; j0 <= pos; j0 += 64) {
-    const uint32_t j = j0 + lane;
-    float sc = -INFINITY;
-    size_t at = 0;
-    bool there = false;
-    if (j <= pos) {
-      there = cache_row(s, slot, kvh, j, &at);
-      if (!there) report_rows(s.err, DE_BAD_PAGE, seq, j);
-      if (there) {
-        sc = 0.f;
-        for (int e = 0; e < D; e += 8) {
-          float kk[8];
-          load8(s.k + at + e, kk);
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), l31 = lane & 31u, half = lane >> 5;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
+  const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
+  const Deal d = deal_units<D>(s, q, lg);
+  const uint32_t total = uniform_u32(d.total);
+  const float scale2 = 1.44269504088896340736f / sqrtf((float)D);   // scores count in powers of two
+
+  for (uint32_t u = blockIdx.x; u < total; u += gridDim.x) {
+    // ---- the unit: sequence, tile of rows (the longest first), run of blocks, KV head (the one that neighbours in time share an L2 for)
+    const uint32_t mine = d.tiles * d.chunks * s.n_kv;
+    const uint32_t seq = (uint32_t)__builtin_ctzll(__ballot(mine && u >= d.first_unit && u < d.first_unit + mine));
+    const uint32_t T = __builtin_amdgcn_readlane((uint32_t)(q.end - q.begin), seq), pos0 = __builtin_amdgcn_readlane(q.pos, seq);
+    const uint32_t slot = __builtin_amdgcn_readlane(q.slot, seq), begin = __builtin_amdgcn_readlane(q.begin, seq);
+    const uint32_t chunks = __builtin_amdgcn_readlane(d.chunks, seq), per = __builtin_amdgcn_readlane(d.blocks, seq);
+    const uint32_t v = u - __builtin_amdgcn_readlane(d.first_unit, seq), kvh = v % s.n_kv, w = v / s.n_kv;
+    const uint32_t chunk = w % chunks, tile = __builtin_amdgcn_readlane(d.tiles, seq) - 1u - w / chunks;
+    const uint32_t nb = tile_blocks(pos0, T, tile, lg), b0 = chunk * per, b1 = min(nb, b0 + per);
+    if (b0 >= b1) continue;
+    const uint32_t rows = T << lg, last = pos0 + T - 1u;   // the sequence's last row in the cache
+    // ---- queries: B operand, lane = row, 8 columns a step and half
+    const uint32_t r = tile * kTileRows + wave * 32u + l31, rr = min(r, rows - 1u), t = rr >> lg;
+    const uint32_t head = (kvh << lg) + (rr & ((1u << lg) - 1u)), pos = pos0 + t;
+    u32x4 qf[KS];
+    {
+      const uint16_t* p = a.q + (size_t)(begin + t) * a.q_stride + (size_t)head * D + 8u * half;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sc = fmaf(qs[e + i], kk[i], sc);
+      for (uint32_t k = 0; k < KS; ++k) qf[k] = *as_global((const u32x4*)(p + 16u * k));
+    }
+    const uint32_t w0 = tile * kTileRows + wave * 32u;   // the wavefront's rows: none behind `rows`
+    const bool have = w0 < rows;
+    const uint32_t pos_lo = pos0 + (min(w0, rows - 1u) >> lg), pos_hi = pos0 + (min(w0 + 31u, rows - 1u) >> lg);
+    const uint32_t tile_lo = pos0 + ((tile * kTileRows) >> lg);
+    // ---- tiles of keys and values: this wavefront's 16 rows of a block
+    const uint16_t *kbase, *vbase;
+    const size_t head_at = PAGED ? ((size_t)kvh << s.page_shift) * D : ((size_t)slot * s.n_kv + kvh) * s.max_seq * D;
+    kbase = s.k + head_at;
+    vbase = s.v + head_at;
+    uint32_t voff[IPW], jrow[IPW];
+#pragma unroll
+    for (uint32_t i = 0; i < IPW; ++i) {
+      jrow[i] = lane / CPR;
+      voff[i] = ((lane % CPR) ^ swizzle<D>(wave * 16u + i * RPI + lane / CPR)) * 16u;
+    }
+    uint32_t page[2] = {0, 0};
+    auto fetch_pages = [&](uint32_t b) {   // of the two runs of 8 rows (a page has 8 at least)
+      if constexpr (PAGED) {
+#pragma unroll
+        for (uint32_t g = 0; g < 2; ++g)
+          page[g] = ld_u32c((const uint32_t*)s.table + (size_t)slot * s.blocks + (min(b * kBlockKeys + wave * 16u + g * 8u, last) >> s.page_shift));
+      }
+    };
+    auto request = [&](uint32_t b, uint32_t buf) {
+      uint32_t pg[2] = {page[0], page[1]};
+      if constexpr (PAGED) {
+#pragma unroll
+        for (uint32_t g = 0; g < 2; ++g)
+          if (pg[g] >= s.n_pages) {
+            if (lane == 0) report_rows(s.err, DE_BAD_PAGE, seq, min(b * kBlockKeys + wave * 16u + g * 8u, last));
+            pg[g] = 0;
+          }
+      }
+      const bool whole = b * kBlockKeys + kBlockKeys - 1u <= last;
+#pragma unroll
+      for (uint32_t i = 0; i < IPW; ++i) {
+        const uint32_t r0 = b * kBlockKeys + wave * 16u + i * RPI, c0 = min(r0, last);
+        // rows behind the last one are the last one: nothing beyond what has been appended is ever read
+        const uint32_t j = whole ? jrow[i] : min(r0 + jrow[i], last) - c0;
+        const size_t at = PAGED ? (((size_t)pg[i * RPI / 8u] * s.n_kv << s.page_shift) + (c0 & ((1u << s.page_shift) - 1u))) * D : (size_t)c0 * D;
+        const uint32_t to = lds0 + buf * 2u * TILE + (wave * IPW + i) * 1024u, off = j * ROWB + voff[i];
+        load_to_lds(kbase + at, off, to);
+        load_to_lds(vbase + at, off, to + TILE);
+      }
+    };
+    fetch_pages(b0);
+    request(b0, 0);
+    fetch_pages(min(b0 + 1u, b1 - 1u));
+
+    f32x16 o[NT];
+#pragma unroll
+    for (uint32_t n = 0; n < NT; ++n) o[n] = f32x16{};
+    float m = -3.402823466e38f, lsum = 0.f;   // of the lane's row (the sum: of the lane's keys)
+    const uint32_t krow = l31 * ROWB, kx = (half ^ swizzle<D>(l31)) * 16u;
+    const uint32_t rl = (lane & 15u) >> 2, un = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
+    drain_vmem();
+    __syncthreads();
+
+    for (uint32_t b = b0; b < b1; ++b) {
+      const uint32_t buf = (b - b0) & 1u, kv0 = b * kBlockKeys;
+      if (b + 1u < b1) {
+        request(b + 1u, buf ^ 1u);
+        fetch_pages(min(b + 2u, b1 - 1u));
+      }
+      const uint32_t kt = lds0 + buf * 2u * TILE, vt = kt + TILE;
+      bool poisoned = false;
+      if (kv0 + kBlockKeys - 1u > tile_lo) {   // some row does not see all of the block
+        // 0 x NaN is NaN: a value that is not finite must not meet the zero probability of a row that does not see it.  Such
+        // values are taken out of the tile and added below to the rows that do.
+        lds_u32* p = (lds_u32*)(uintptr_t)(vt + threadIdx.x * (TILE / 256u));
+        uint32_t bad = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < TILE / 1024u; ++i) bad |= nonfinite(p[i]);
+        if (threadIdx.x == 0) any_bad = 0;
+        __syncthreads();
+        if (bad) any_bad = 1;
+        __syncthreads();
+        poisoned = any_bad != 0;
+        if (poisoned) {
+          for (uint32_t i = 0; i < TILE / 1024u; ++i) {
+            const uint32_t x = p[i], n = nonfinite(x);
+            p[i] = x & ~(((n & 0x8000u) ? 0xFFFFu : 0u) | ((n & 0x80000000u) ? 0xFFFF0000u : 0u));
+          }
+          __syncthreads();
         }
-        sc *= 1.0f / sqrtf((float)D);
+      }
+      if (have && kv0 <= pos_hi) {
+        f32x16 sc[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+        for (uint32_t k = 0; k < KS; ++k) {
+#pragma unroll
+          for (uint32_t n = 0; n < 2; ++n) {
+            const u32x4 kf = *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(kt + ((krow + kx) ^ (32u * k)) + n * 32u * ROWB);
+            sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), sc[n], 0, 0, 0);
+          }
+        }
+        if (kv0 + kBlockKeys - 1u > pos_lo) {
+#pragma unroll
+          for (uint32_t n = 0; n < 2; ++n)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+              if (kv0 + 32u * n + 8u * (i >> 2) + 4u * half + (i & 3u) > pos) sc[n][i] = -INFINITY;
+        }
+        float mx = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+        for (uint32_t i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        if (__any(mx > m)) {
+          const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f((m - mn) * scale2);
+          lsum *= f;
+          m = mn;
+#pragma unroll
+          for (uint32_t n = 0; n < NT; ++n) o[n] *= f;
+        }
+        const float ms = m * scale2;
+        bf16x8 pf[4];
+#pragma unroll
+        for (uint32_t n = 0; n < 2; ++n)
+#pragma unroll
+          for (uint32_t i = 0; i < 16; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][i], scale2, -ms));
+            lsum += p;
+            pf[2 * n + (i >> 3)][i & 7u] = (__bf16)p;
+          }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+          for (uint32_t n = 0; n < NT; ++n) {
+            union { s16x4 h[2]; bf16x8 v; } vf;
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x) {
+              const uint32_t place = D == 128 ? ((n ^ rl) << 2) | (un ^ (half + 2u * x)) : ((n ^ (rl >> 1)) << 2) | (un ^ (half + 2u * x));
+              const uint32_t at = vt + (16u * k + 8u * x + 4u * half + rl) * ROWB + place * 16u + 8u * (lane & 1u);
+              vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
+            }
+            o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[k], o[n], 0, 0, 0);
+          }
+        if (poisoned) {
+          for (uint32_t j = 0; j < kBlockKeys && kv0 + j <= pos_hi; ++j) {
+            size_t at = 0;
+            if (!cache_row(s, slot, kvh, kv0 + j, &at) || kv0 + j > pos) continue;
+#pragma unroll
+            for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                const uint32_t x = as_global(s.v)[at + 32u * n + 8u * (i >> 2) + 4u * half + (i & 3u)];
+                if ((x & 0x7F80u) == 0x7F80u) o[n][i] += bf16_to_f32((uint16_t)x);
+              }
+          }
+        }
+      }
+      drain_vmem();
+      __syncthreads();
+    }
+    // ---- the end: the row's sum of both halves; the output, or the unit's partial result
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+    const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (r < rows) {
+      if (nb <= per) {
+        const float inv = 1.0f / l;
+        uint16_t* to = a.out + (size_t)(begin + t) * a.out_stride + (size_t)head * D + 4u * half;
+#pragma unroll
+        for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            const u32x2 x = {pack_bf16(o[n][4 * i] * inv, o[n][4 * i + 1] * inv), pack_bf16(o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv)};
+            *as_global((u32x2*)(to + 32u * n + 8u * i)) = x;
+          }
+      } else {
+        const uint32_t held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
+        float* part = (float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)v * held * (D + 2u);
+        float* to = part + (size_t)in_tile * D + 4u * half;
+#pragma unroll
+        for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) *as_global((f32x4*)(to + 32u * n + 8u * i)) = f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+        if (half == 0) *as_global((f32x2*)(part + (size_t)held * D + 2u * in_tile)) = f32x2{m * scale2, l};
       }
     }
-    const float mn = fmaxf(m, wave_max(sc)), scale = m == mn ? 1.f : expf(m - mn);
-    const float p = sc == -INFINITY ? 0.f : expf(sc - mn);
-    l = l * scale + wave_sum(p);
-    m = mn;
-    ps[lane] = p;
-    vat[lane] = there ? at : ~0ull;
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      o[c] *= scale;
-      for (int i = 0; i < 64; ++i)
-        if (vat[i] != ~0ull) o[c] = fmaf(ps[i], bf16_to_f32(as_global(s.v)[vat[i] + c * 64 + lane]), o[c]);
-    }
-    __syncthreads();
   }
+}
+
+// Joins the partial results of a row whose tile was cut into runs, in their order: a wavefront per row and query head.
+template <int D>
+__global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uint32_t lg) {
+  const RowSeqs& s = a.s;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
+  const SeqLanes q = load_seqs(s, false);
+  const Deal d = deal_units<D>(s, q, lg);
+  const uint32_t item = blockIdx.x * 4u + wave, row = item / s.n_q, head = item - row * s.n_q;
+  if (row >= s.n_rows) return;
+  const uint32_t seq = seq_of_row(q, row);
+  if (seq == 64u) return;
+  const uint32_t T = __builtin_amdgcn_readlane((uint32_t)(q.end - q.begin), seq), pos0 = __builtin_amdgcn_readlane(q.pos, seq);
+  const uint32_t chunks = __builtin_amdgcn_readlane(d.chunks, seq), per = __builtin_amdgcn_readlane(d.blocks, seq);
+  const uint32_t r = ((row - __builtin_amdgcn_readlane(q.begin, seq)) << lg) + (head & ((1u << lg) - 1u)), tile = r / kTileRows;
+  const uint32_t n = (tile_blocks(pos0, T, tile, lg) + per - 1u) / per;
+  if (n <= 1u) return;
+  const uint32_t rows = T << lg, held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
+  const uint32_t v0 = (__builtin_amdgcn_readlane(d.tiles, seq) - 1u - tile) * chunks * s.n_kv + (head >> lg);
+  const float* part = (const float*)a.work + __builtin_amdgcn_readlane(d.part, seq);
+  const size_t stride = (size_t)s.n_kv * held * (D + 2u);
+  part += (size_t)v0 * held * (D + 2u);
+  float M = -INFINITY;
+  for (uint32_t c = 0; c < n; ++c) M = fmaxf(M, as_global(part)[c * stride + (size_t)held * D + 2u * in_tile]);
+  float l = 0.f, o[D / 64] = {};
+  for (uint32_t c = 0; c < n; ++c) {
+    const float* p = part + c * stride;
+    const f32x2 ml = *as_global((const f32x2*)(p + (size_t)held * D + 2u * in_tile));
+    const float f = __builtin_amdgcn_exp2f(ml.x - M);
+    l = fmaf(ml.y, f, l);
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c) as_global(a.out)[(size_t)row * a.out_stride + (size_t)h * D + c * 64 + lane] = f32_to_bf16(o[c] / l);
+    for (int e = 0; e < D / 64; ++e) o[e] = fmaf(as_global(p)[(size_t)in_tile * D + (D / 64) * lane + e], f, o[e]);
+  }
+  const float inv = 1.0f / l;
+  uint16_t* to = a.out + (size_t)row * a.out_stride + (size_t)head * D + (D / 64) * lane;
+  if constexpr (D == 128) *as_global((uint32_t*)to) = pack_bf16(o[0] * inv, o[1] * inv);
+  else *as_global(to) = f32_to_bf16(o[0] * inv);
+}
+
+constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
+hipError_t rows_prepare() {
+  hipError_t e = hipSuccess;
+  for (const void* fn : {(const void*)rows_attend_kernel<128, false>, (const void*)rows_attend_kernel<128, true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_lds(128));
+  return e;
+}
+
+template <int D, bool PAGED>
+static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t stream) {
+  const uint64_t tiles = (((uint64_t)a.s.n_rows << lg) / kTileRows + a.s.n_seqs) * a.s.n_kv;
+  rows_attend_kernel<D, PAGED><<<dim3((uint32_t)std::min<uint64_t>(tiles + 2u * kAttendSlots, 1u << 20)), dim3(256), attend_lds(D), stream>>>(a, lg);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  rows_attend_join_kernel<D><<<dim3((uint32_t)(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u)), dim3(256), 0, stream>>>(a, lg);
+  return hipGetLastError();
 }
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
-  const dim3 grid(a.s.n_rows * a.s.n_q);
-  if (a.s.head_dim == 128u) rows_attend_kernel<128><<<grid, dim3(64), 0, stream>>>(a);
-  else rows_attend_kernel<64><<<grid, dim3(64), 0, stream>>>(a);
-  return hipGetLastError();
+  uint32_t lg = 0;
+  while ((1u << lg) < a.s.n_q / a.s.n_kv) ++lg;
+  if (a.s.head_dim == 128u) return a.s.table ? launch_attend<128, true>(a, lg, stream) : launch_attend<128, false>(a, lg, stream);
+  return a.s.table ? launch_attend<64, true>(a, lg, stream) : launch_attend<64, false>(a, lg, stream);
 }
 
 // ------------------------------------------------------------------------------------ log probabilities

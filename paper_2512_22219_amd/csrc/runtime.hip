@@ -516,6 +516,7 @@ extern "C" mpk_status mpk_compile(const mpk_model_config* cfg, const mpk_weight_
       if ((st = upload(&g->d_const_static, csv)) != MPK_OK) return fail(st);
     }
   }
+  if ((e = rows_prepare()) != hipSuccess) { set_error("cannot reserve LDS for the calls on rows: %s", hipGetErrorString(e)); return fail(MPK_ERR_HIP); }
   g->cache_k = (uint16_t*)kv->k;
   g->cache_v = (uint16_t*)kv->v;
   const bool qk_norm = (cfg->flags & MPK_MODEL_QK_NORM) != 0;
