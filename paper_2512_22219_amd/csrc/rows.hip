@@ -192,7 +192,8 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 // K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
-constexpr uint32_t kAttendMinBlocks = 2;
+constexpr uint32_t kJoinWorkgroups = 2048;
+constexpr uint32_t kAttendMinBlocks = 2, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -219,6 +220,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
     work += (uint64_t)__builtin_amdgcn_readlane(d.tiles, i) *
             (((uint32_t)__builtin_amdgcn_readlane(q.pos, i) + (uint32_t)__builtin_amdgcn_readlane(T, i) / 2u) / kBlockKeys + 1u);
   uint32_t c = (uint32_t)max((uint64_t)kAttendMinBlocks, (work * s.n_kv + kAttendSlots - 1u) / kAttendSlots);
+  c = max(c, (s.max_seq + kBlockKeys * kAttendMostChunks - 1u) / (kBlockKeys * kAttendMostChunks));
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace)
     d.chunks = nb > c ? (nb + c - 1u) / c : 1u;
     const float need = d.chunks > 1u ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(min(rows, kTileRows) * (D + 2u)) : 0.f;
@@ -483,35 +485,65 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
   const SeqLanes q = load_seqs(s, false);
   const Deal d = deal_units<D>(s, q, lg);
-  const uint32_t item = blockIdx.x * 4u + wave, row = item / s.n_q, head = item - row * s.n_q;
-  if (row >= s.n_rows) return;
+  if (!__ballot(d.chunks > 1u)) return;
+  for (uint64_t item = blockIdx.x * 4u + wave; item < (uint64_t)s.n_rows * s.n_q; item += gridDim.x * 4u) {
+  const uint32_t row = (uint32_t)(item / s.n_q), head = (uint32_t)(item - (uint64_t)row * s.n_q);
   const uint32_t seq = seq_of_row(q, row);
-  if (seq == 64u) return;
+  if (seq == 64u) continue;
   const uint32_t T = __builtin_amdgcn_readlane((uint32_t)(q.end - q.begin), seq), pos0 = __builtin_amdgcn_readlane(q.pos, seq);
   const uint32_t chunks = __builtin_amdgcn_readlane(d.chunks, seq), per = __builtin_amdgcn_readlane(d.blocks, seq);
   const uint32_t r = ((row - __builtin_amdgcn_readlane(q.begin, seq)) << lg) + (head & ((1u << lg) - 1u)), tile = r / kTileRows;
   const uint32_t n = (tile_blocks(pos0, T, tile, lg) + per - 1u) / per;
-  if (n <= 1u) return;
+  if (n <= 1u) continue;
   const uint32_t rows = T << lg, held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
   const uint32_t v0 = (__builtin_amdgcn_readlane(d.tiles, seq) - 1u - tile) * chunks * s.n_kv + (head >> lg);
-  const float* part = (const float*)a.work + __builtin_amdgcn_readlane(d.part, seq);
   const size_t stride = (size_t)s.n_kv * held * (D + 2u);
-  part += (size_t)v0 * held * (D + 2u);
-  float M = -INFINITY;
-  for (uint32_t c = 0; c < n; ++c) M = fmaxf(M, as_global(part)[c * stride + (size_t)held * D + 2u * in_tile]);
-  float l = 0.f, o[D / 64] = {};
-  for (uint32_t c = 0; c < n; ++c) {
-    const float* p = part + c * stride;
-    const f32x2 ml = *as_global((const f32x2*)(p + (size_t)held * D + 2u * in_tile));
-    const float f = __builtin_amdgcn_exp2f(ml.x - M);
-    l = fmaf(ml.y, f, l);
+  const float* part = (const float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)v0 * held * (D + 2u);
+  // a lane holds maximum and sum of the runs lane, lane + 64, ..; then all loads of a stretch of runs are in flight at once
+  float m[kAttendMostChunks / 64], w[kAttendMostChunks / 64], M = -INFINITY, l = 0.f, o[D / 64] = {};
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) o[e] = fmaf(as_global(p)[(size_t)in_tile * D + (D / 64) * lane + e], f, o[e]);
+  for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
+    m[i] = -INFINITY;
+    w[i] = 0.f;
+    if (64u * i + lane < n) {
+      const f32x2 ml = *as_global((const f32x2*)(part + (64u * i + lane) * stride + (size_t)held * D + 2u * in_tile));
+      m[i] = ml.x;
+      w[i] = ml.y;
+    }
+    M = fmaxf(M, m[i]);
+  }
+  M = wave_max_dpp(M);
+#pragma unroll
+  for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
+    const float f = __builtin_amdgcn_exp2f(m[i] - M);
+    l = fmaf(w[i], f, l);
+    w[i] = f;
+  }
+  l = wave_sum_dpp(l);
+  const float* p = part + (size_t)in_tile * D + (D / 64) * lane;
+#pragma unroll
+  for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
+    if (64u * i >= n) break;
+    const uint32_t here = min(64u, n - 64u * i);
+    for (uint32_t c = 0; c < here; c += 8u) {
+      float v[8][D / 64];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(64u * i + c + j, n - 1u) * stride + e];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        const float f = c + j < here ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[i]), (c + j) & 63u)) : 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) o[e] = c + j < here ? fmaf(v[j][e], f, o[e]) : o[e];
+      }
+    }
   }
   const float inv = 1.0f / l;
   uint16_t* to = a.out + (size_t)row * a.out_stride + (size_t)head * D + (D / 64) * lane;
   if constexpr (D == 128) *as_global((uint32_t*)to) = pack_bf16(o[0] * inv, o[1] * inv);
   else *as_global(to) = f32_to_bf16(o[0] * inv);
+  }
 }
 
 constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
@@ -528,7 +560,7 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   rows_attend_kernel<D, PAGED><<<dim3((uint32_t)std::min<uint64_t>(tiles + 2u * kAttendSlots, 1u << 20)), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  rows_attend_join_kernel<D><<<dim3((uint32_t)(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u)), dim3(256), 0, stream>>>(a, lg);
+  rows_attend_join_kernel<D><<<dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
   return hipGetLastError();
 }
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
@@ -539,79 +571,347 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------ log probabilities
+// One pass over a row.  A wavefront reads 16 logits a lane and step and keeps, against the largest m that it has seen,
+//   s = sum e^(x - m) without one of the largest, t = sum e^(x - m) (x - m)
+// (ln p = x - m - log1p(s): nothing is lost of a token that is all but certain; entropy = log1p(s) - t / (1 + s)), and its
+// best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
+// With few rows a row is cut into runs of steps, one a workgroup, and a second kernel joins these.
+constexpr uint32_t kStep = 1024;          // logits of a wavefront's step
+constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
+constexpr uint32_t kLogprobWorkgroups = 1024;   // that a call is cut into where its rows are fewer
+constexpr uint32_t kLogprobManyRows = 2048;     // a wavefront a row from here on
+
+// A logit and its token as one number: larger logits first, of equal ones the lower token.  0: none.
+__device__ __forceinline__ uint64_t entry_of(float x, uint32_t token) {
+  const uint32_t u = __float_as_uint(x + 0.0f);   // (-0 is 0)
+  return ((uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (0xFFFFFFFFu - token);
+}
+__device__ __forceinline__ float entry_logit(uint64_t e) {
+  const uint32_t k = (uint32_t)(e >> 32);
+  return __uint_as_float(k ^ ((k & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+struct RowSum {
+  float m, s, t;
+};
+// The sums of the wavefront's first n lanes, as one (in every lane).
+__device__ __forceinline__ RowSum join_sums(const RowSum& a, uint32_t n) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const float mine = lane < n ? a.m : -INFINITY, m = wave_max_dpp(mine);
+  const uint64_t holds = __ballot(lane < n && a.m == m);
+  float s = 0.f, t = 0.f;
+  if (holds && lane == (uint32_t)__builtin_ctzll(holds)) { s = a.s; t = a.t; }
+  else if (lane < n) {
+    if (a.m == -INFINITY) s = a.s;   // (nothing: 0, or NaN)
+    else {
+      const float d = fmaxf(a.m - m, -200.f), f = __expf(d);
+      s = (a.s + 1.f) * f;
+      t = (a.t + (a.s + 1.f) * d) * f;
+    }
+  }
+  return RowSum{m, wave_sum_dpp(s), wave_sum_dpp(t)};
+}
+
+// The best k of n entries in LDS, in order, into best [k] (empty before).  The whole workgroup calls it.
+__device__ __forceinline__ void rank_entries(const uint64_t* list, uint32_t n, uint32_t k, uint64_t* best) {
+  for (uint32_t i = threadIdx.x; i < n; i += 256u) {
+    const uint64_t mine = list[i];
+    uint32_t rank = 0;
+#pragma unroll 8
+    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine;
+    if (mine && rank < k) best[rank] = mine;
+  }
+}
+
+// What is written for a row, by one wavefront: `mine` is lane j's j-th best entry, empty ones last.
+__device__ __forceinline__ void write_row(const LogprobArgs& a, uint32_t row, const RowSum& r, float asked, uint64_t mine) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const bool none = !(r.m > -INFINITY) || r.m == INFINITY || r.s != r.s;
+  const float norm = log1pf(r.s), nan = __uint_as_float(0x7FC00000u);
+  if (lane == 0) {
+    if (a.entropy) as_global(a.entropy)[row] = none ? nan : norm - r.t / (1.f + r.s);
+    if (a.tokens) {
+      const int32_t t = as_global(a.tokens)[row];
+      float lp = nan;
+      if (t == -1) lp = 0.f;
+      else if (t < 0 || (uint32_t)t >= a.vocab) report_rows(a.err, DE_BAD_TOKEN, row, (uint32_t)t);
+      else if (!none) lp = asked - r.m - norm;
+      as_global(a.logprobs)[row] = lp;
+    }
+  }
+  if (!a.n_top) return;
+  mine = lane < a.n_top ? mine : 0;
+  const uint32_t real = (uint32_t)__popcll(__ballot(mine != 0));
+  uint32_t id = 0xFFFFFFFFu - (uint32_t)mine;
+  if (real < a.n_top) {   // fewer tokens above -inf than asked for: the lowest of the others
+    bool listed = false;
+    for (uint32_t j = 0; j < real; ++j) listed |= (uint32_t)__builtin_amdgcn_readlane((int)id, j) == lane;
+    uint32_t at = real;
+    for (uint64_t b = __ballot(!listed); b && at < a.n_top; b &= b - 1, ++at)
+      if (lane == at) id = (uint32_t)__builtin_ctzll(b);
+  }
+  if (lane < a.n_top) {
+    as_global(a.top_tokens)[(size_t)row * a.n_top + lane] = none ? -1 : (int32_t)id;
+    as_global(a.top_logprobs)[(size_t)row * a.n_top + lane] = none ? nan : (mine ? entry_logit(mine) : -INFINITY) - r.m - norm;
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ float logit_at(const T* p, size_t i) {
   if constexpr (sizeof(T) == 4) return as_global(p)[i];
   else return bf16_to_f32(as_global(p)[i]);
 }
-// One workgroup per row, a pass for the largest, one for the sums, one for each alternative.
+// The logit asked about, 0 for no token or a wrong one.
 template <typename T>
-__global__ void __launch_bounds__(512) rows_logprobs_kernel(LogprobArgs a) {
-  __shared__ float red[16];
-  __shared__ uint64_t best[8];
-  const uint32_t row = blockIdx.x, tid = threadIdx.x;
+__device__ __forceinline__ float asked_logit(const LogprobArgs& a, uint32_t row) {
+  if (!a.tokens) return 0.f;
+  const int32_t t = as_global(a.tokens)[row];
+  return t >= 0 && (uint32_t)t < a.vocab ? logit_at((const T*)a.logits + (size_t)row * a.stride, (size_t)t) : 0.f;
+}
+
+// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [128]) and
+// joined with them 64 at a time: an entry's place is the number of entries above it.  (Put in place one by one, the lanes
+// behind shifted, a row of 151936 with 20 alternatives took 18.8 us instead of 8.7, 4096 rows of 32000 with 4 106 instead of 94.)
+struct Best {
+  uint64_t mine = 0, last = 0;   // last: the n_top-th, 0 while there are fewer
+  uint32_t count = 0, waiting = 0;
+  __device__ __forceinline__ void join(uint64_t* fresh, uint64_t* sorted, uint32_t n_top) {
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint32_t at = 0; at < waiting; at += 64u) {
+      const uint32_t n = min(64u, waiting - at);
+      const uint64_t now = lane < n ? fresh[at + lane] : 0;
+      uint32_t place_now = 0, place_old = lane;
+      for (uint32_t i = 0; i < n; ++i) {
+        const uint64_t e = readlane64(now, i);
+        place_now += e > now;
+        place_old += e > mine;
+      }
+      for (uint32_t i = 0; i < count; ++i) place_now += readlane64(mine, i) > now;
+      if (lane < n && place_now < n_top) sorted[place_now] = now;
+      if (lane < count && place_old < n_top) sorted[place_old] = mine;
+      count = min(n_top, count + n);
+      mine = lane < count ? sorted[lane] : 0;
+    }
+    waiting = 0;
+    last = count == n_top ? readlane64(mine, n_top - 1u) : 0;
+  }
+};
+
+// W wavefronts of a workgroup share a run (4, or 1: a run each).
+template <typename T, uint32_t W>
+__global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t steps) {
+  constexpr uint32_t E = 16 / sizeof(T), V = 16 / E;   // logits of 16 bytes, such loads of a step
+  __shared__ uint64_t fresh[4][128], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
+  __shared__ __align__(16) float offered[4][64][20];   // (20: reads of 16 logits of four lanes spread over the banks)
+  __shared__ RowSum sums[4];
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), part_of = W == 1 ? 0u : wave;
+  const uint32_t unit = W == 1 ? blockIdx.x * 4u + wave : blockIdx.x, row = unit / chunks, chunk = unit - row * chunks, k = a.n_top;
+  if (W == 1 && row >= a.n_rows) return;
   const T* x = (const T*)a.logits + (size_t)row * a.stride;
-  float m = -INFINITY, bad = 0.f;
-  for (uint32_t i = tid; i < a.vocab; i += 512) {
-    const float v = logit_at(x, i);
-    if (!(v < INFINITY)) bad = 1.f;
-    m = fmaxf(m, v);
+  const uint32_t head = min(a.vocab, (uint32_t)((16u - ((uintptr_t)x & 15u)) & 15u) / (uint32_t)sizeof(T));   // logits in front of a 16-byte boundary
+  const uint32_t nvec = (a.vocab - head) / E, tail = a.vocab - head - nvec * E;
+  const MPK_GLOBAL u32x4* xv = (const MPK_GLOBAL u32x4*)(x + head);
+  const uint32_t v0 = chunk * steps * (kStep / E), v1 = min(nvec, v0 + steps * (kStep / E));
+  float asked = 0.f;
+
+  RowSum r = {-INFINITY, 0.f, 0.f};
+  Best best;
+  float limit = -INFINITY;   // the last of the best (nothing to beat without alternatives but the largest)
+  u32x4 next[V];
+  auto request = [&](uint32_t first) {
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) next[j] = xv[min(first + j * 64u + lane, v1 - 1u)];
+  };
+  uint32_t at = v0 + part_of * (kStep / E);
+  if (at < v1) request(at);
+  if (chunks == 1u && part_of == 0) asked = asked_logit<T>(a, row);
+  // The row's edges, what lies in front of the first and behind the last load of 16 bytes, come last, as one step.
+  bool edges = false;
+  for (;;) {
+    float y[16];
+    const uint32_t first = at;
+    if (at < v1) {
+      u32x4 now[V];
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) now[j] = next[j];
+      at += W * (kStep / E);
+      if (at < v1) request(at);
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          if constexpr (E == 4) y[4 * j + e] = __uint_as_float(now[j][e]);
+          else { y[8 * j + 2 * e] = bf16_lo(now[j][e]); y[8 * j + 2 * e + 1] = bf16_hi(now[j][e]); }
+        }
+      if (first + kStep / E > v1) {
+#pragma unroll
+        for (uint32_t j = 0; j < 16; ++j)
+          if (first + (j / E) * 64u + lane >= v1) y[j] = -INFINITY;
+      }
+    } else {
+      if (edges || chunk || part_of || !(head + tail)) break;
+      edges = true;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] = -INFINITY;
+      if (lane < head + tail) y[0] = logit_at(x, lane < head ? lane : a.vocab - tail + (lane - head));
+    }
+    float mx = y[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) mx = fmaxf(mx, y[j]);
+    // (tokens ascend, so an equal logit does not beat one; the edges come out of order)
+    uint64_t hot = __ballot(mx > limit || (edges && mx == limit));
+    if (hot) {
+      const float m = wave_max_dpp(mx);
+      const bool more = m > r.m;
+      if (more) {
+        if (r.m != -INFINITY) {
+          const float d = fmaxf(r.m - m, -200.f), f = __expf(d);
+          if (lane == 0) r.s += 1.f;   // the largest until now is one of many
+          r.t = fmaf(r.s, d, r.t) * f;
+          r.s *= f;
+        }
+        r.m = m;
+      }
+      if (k) {
+        float least = -3.402823466e38f;
+        if ((uint32_t)__popcll(hot) > k) {
+          // more lanes than places: k logits are at or above the k-th largest of the lanes' largest (its upper 16 bits)
+          const uint32_t key = mx == mx ? (uint32_t)(entry_of(mx, 0) >> 32) : 0u;
+          uint32_t p = 0;
+          for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
+            if ((uint32_t)__popcll(__ballot(key >= (p | bit))) >= k) p |= bit;
+          if (p > 0x007FFFFFu) least = fmaxf(least, entry_logit((uint64_t)p << 32));
+          hot = __ballot(mx >= least);
+        }
+        if (hot >> lane & 1u) {
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) *(float4*)&offered[wave][lane][j] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+        }
+        while (hot) {   // four such lanes at a time
+          uint32_t from = 64u;
+#pragma unroll
+          for (uint32_t g = 0; g < 4; ++g) {
+            if (hot && lane >> 4 == g) from = (uint32_t)__builtin_ctzll(hot);
+            hot &= hot - 1ull;
+          }
+          const uint32_t j = lane & 15u;
+          const float v = from < 64u ? offered[wave][from & 63u][j] : -INFINITY;
+          const uint32_t token = edges ? (from < head ? from : a.vocab - tail + (from - head)) : head + (first + (j / E) * 64u + from) * E + j % E;
+          const uint64_t e = entry_of(v, token), b = __ballot(v >= least && e > best.last);
+          if (!b) continue;
+          if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
+          best.waiting += (uint32_t)__popcll(b);
+          if (best.waiting >= 64u) best.join(fresh[wave], sorted[wave], k);
+        }
+        if (best.waiting) best.join(fresh[wave], sorted[wave], k);
+        limit = best.last ? entry_logit(best.last) : -INFINITY;
+      } else limit = r.m;
+      if (more) {   // one of the largest stays out of the sum
+        bool out = lane == (uint32_t)__builtin_ctzll(__ballot(mx == m));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const bool it = out && y[j] == m;
+          y[j] = it ? -INFINITY : y[j];
+          out = out && !it;
+        }
+      }
+    }
+    const float m = r.m == -INFINITY ? 0.f : r.m;
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float d = y[j] - m, e = __expf(d);
+      s += e;
+      t = fmaf(e, fmaxf(d, -200.f), t);
+    }
+    r.s += s;
+    r.t += t;
   }
-  bad = block_sum(bad, red);
-  m = wave_max(m);
-  __syncthreads();
-  if ((tid & 63) == 0) red[tid >> 6] = m;
-  __syncthreads();
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, red[i]);
-  float sum = 0.f, dot = 0.f;
-  for (uint32_t i = tid; i < a.vocab; i += 512) {
-    const float d = fmaxf(logit_at(x, i) - m, -200.f), e = expf(d);
-    sum += e;
-    dot = fmaf(e, d, dot);
+  // ---- the lanes' and the wavefronts' results together
+  r.s = wave_sum_dpp(r.s);
+  r.t = wave_sum_dpp(r.t);
+  uint64_t mine = best.mine;
+  if constexpr (W > 1) {
+    if (lane == 0) sums[wave] = r;
+    if (lane < k) list[wave * k + lane] = mine;
+    if (wave == 1 && lane < k) first_best[lane] = 0;
+    __syncthreads();
+    if (k) {
+      rank_entries(list, 4u * k, k, first_best);
+      __syncthreads();
+    }
+    if (wave) return;
+    r = join_sums(sums[lane & 3u], 4);
+    if (lane < k) mine = first_best[lane];
   }
-  sum = block_sum(sum, red);
-  dot = block_sum(dot, red);
-  const bool none = bad != 0.f || m == -INFINITY;
-  const float norm = logf(sum), nan = __uint_as_float(0x7FC00000u);
-  if (tid == 0) {
-    if (a.entropy) a.entropy[row] = none ? nan : norm - dot / sum;
-    if (a.tokens) {
-      const int32_t t = a.tokens[row];
-      float lp = nan;
-      if (t == -1) lp = 0.f;
-      else if (t < 0 || (uint32_t)t >= a.vocab) report_rows(a.err, DE_BAD_TOKEN, row, (uint32_t)t);
-      else if (!none) lp = logit_at(x, (uint32_t)t) - m - norm;
-      a.logprobs[row] = lp;
+  if (chunks == 1u) { write_row(a, row, r, asked, mine); return; }
+  uint64_t* part = (uint64_t*)a.work + (size_t)unit * (2u + k);
+  if (lane == 0) { as_global((float*)part)[0] = r.m; as_global((float*)part)[1] = r.s; as_global((float*)part)[2] = r.t; }
+  if (lane < k) as_global(part)[2 + lane] = mine;
+}
+
+// Joins the runs of a row: a workgroup each.
+template <typename T>
+__global__ void __launch_bounds__(256) rows_logprobs_join_kernel(LogprobArgs a, uint32_t chunks) {
+  __shared__ uint64_t list[kLogprobChunks * MPK_ROWS_MAX_TOP], best[MPK_ROWS_MAX_TOP], least;
+  __shared__ uint32_t n;
+  const uint32_t lane = threadIdx.x & 63u, row = blockIdx.x, k = a.n_top, size = 2u + k;
+  const uint64_t* part = (const uint64_t*)a.work + (size_t)row * chunks * size;
+  RowSum r = {-INFINITY, 0.f, 0.f};
+  float asked = 0.f;
+  if (threadIdx.x < 64u) {
+    if (k) {
+      // ceil(k / nth) runs have nth entries at or above the one that this many runs' nth entries are not below: k of the row
+      // are, and few others where about half of the runs have one
+      const uint32_t nth = min(k, (2u * k + chunks - 1u) / chunks), at = (k + nth - 1u) / nth;
+      const uint64_t mine = lane < chunks ? as_global(part)[lane * size + 1u + nth] : 0;
+      uint32_t above = 0;
+      for (uint32_t i = 0; i < chunks; ++i) above += readlane64(mine, i) > mine;
+      const uint64_t holds = __ballot(mine && above == at - 1u);
+      if (lane == 0) { least = 0; n = 0; }
+      if (holds && lane == (uint32_t)__builtin_ctzll(holds)) least = mine;
+      if (lane < k) best[lane] = 0;
+    }
+    asked = asked_logit<T>(a, row);
+    if (lane < chunks) {
+      const MPK_GLOBAL float* p = (const MPK_GLOBAL float*)(part + lane * size);
+      r.m = p[0]; r.s = p[1]; r.t = p[2];
     }
   }
-  uint64_t last = ~0ull;
-  for (uint32_t k = 0; k < a.n_top; ++k) {
-    uint64_t b = 0;
-    for (uint32_t i = tid; i < a.vocab; i += 512) {
-      const uint32_t u = __float_as_uint(logit_at(x, i) + 0.0f);
-      const uint64_t key = ((uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (0xFFFFFFFFu - i);
-      if (key < last && key > b) b = key;
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t other = __shfl_xor((unsigned long long)b, o, 64);
-      b = other > b ? other : b;
+  if (k) {
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < chunks * k; i += 256u) {
+      const uint32_t c = i / k;
+      const uint64_t e = as_global(part)[c * size + 2u + (i - c * k)];
+      if (e && e >= least) list[atomicAdd(&n, 1u)] = e;   // (in any order: an entry's rank goes by all of them)
     }
     __syncthreads();
-    if ((tid & 63) == 0) best[tid >> 6] = b;
+    rank_entries(list, n, k, best);
     __syncthreads();
-    for (int i = 0; i < 8; ++i) b = best[i] > b ? best[i] : b;
-    last = b;
-    if (tid == 0) {
-      const uint32_t i = 0xFFFFFFFFu - (uint32_t)b;
-      a.top_tokens[(size_t)row * a.n_top + k] = none ? -1 : (int32_t)i;
-      a.top_logprobs[(size_t)row * a.n_top + k] = none ? nan : logit_at(x, i) - m - norm;
-    }
   }
+  if (threadIdx.x < 64u) write_row(a, row, join_sums(r, chunks), asked, lane < k ? best[lane] : 0);
+}
+
+template <typename T>
+static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
+  // a workgroup's share: a whole row where there are rows enough for all compute units, 4096 logits or more
+  if (a.n_rows >= kLogprobManyRows) {
+    rows_logprobs_kernel<T, 1><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, (a.vocab + kStep - 1u) / kStep + 1u);
+    return hipGetLastError();
+  }
+  const uint32_t all = std::max(1u, (a.vocab + 4u * kStep - 1u) / (4u * kStep)), want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
+  const uint32_t n = std::min(std::min(want, all), kLogprobChunks), steps = 4u * ((all + n - 1u) / n), chunks = (4u * all + steps - 1u) / steps;
+  rows_logprobs_kernel<T, 4><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, steps);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || chunks == 1u) return e;
+  rows_logprobs_join_kernel<T><<<dim3(a.n_rows), dim3(256), 0, stream>>>(a, chunks);
+  return hipGetLastError();
 }
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream) {
-  if (f32) rows_logprobs_kernel<float><<<dim3(a.n_rows), dim3(512), 0, stream>>>(a);
-  else rows_logprobs_kernel<uint16_t><<<dim3(a.n_rows), dim3(512), 0, stream>>>(a);
-  return hipGetLastError();
+  return f32 ? launch_logprobs<float>(a, stream) : launch_logprobs<uint16_t>(a, stream);
 }
 
 }  // namespace mpk
