@@ -550,8 +550,8 @@ void mpk_serve_destroy(mpk_server *s);
  *     one graph of a set work alike (a set's graph sees the first `batch` slots).
  *   - asynchronous on `stream`; no allocation, no host synchronisation; may be captured into a HIP
  *     graph (all lengths are read from device memory when the work runs, so a replay follows them).
- *   - calls on one graph, decode steps included, must not overlap in time where one of them writes
- *     what the other reads or writes: cache rows, outputs, workspaces.
+ *   - calls on one graph must not overlap in time, decode steps included (same stream, or externally
+ *     ordered), replays of captured ones among them: they share the graph's arrival counters and cache.
  *   - what only the device can see (a row list that does not ascend, a position, slot, page or token
  *     out of range) is reported by mpk_graph_status as MPK_ERR_DEVICE, never dereferenced; the
  *     sequence or row concerned is left out (details below).  The error word keeps the first error
@@ -561,8 +561,8 @@ void mpk_serve_destroy(mpk_server *s);
 typedef enum { MPK_ROWS_BF16 = 0, MPK_ROWS_F32 = 1 } mpk_rows_type;
 
 /* Device memory that mpk_rows_attend and mpk_rows_logprobs work in, given by the caller (16-byte
- * aligned, contents of no matter before and after).  Calls that may overlap in time, replays of captured
- * ones among them, need one each. */
+ * aligned, contents of no matter before and after).  Calls on different graphs that may overlap in
+ * time, replays of captured ones among them, need one each. */
 #define MPK_ROWS_WORKSPACE_BYTES (96u << 20)
 
 /* Query/key norm (MPK_MODEL_QK_NORM), position rotation, append to the KV cache.

@@ -43,7 +43,7 @@ __device__ __forceinline__ SeqLanes load_seqs(const RowSeqs& s, bool tell) {
       what = q.pos < 0 || (uint32_t)q.pos >= s.max_seq ? (uint32_t)q.pos : s.max_seq;
     }
   }
-  for (uint32_t i = 0; i + 1 < s.n_seqs; ++i) {   // (a slot that an earlier sequence with rows has)
+  for (uint32_t i = 0; s.slots && i + 1 < s.n_seqs; ++i) {   // (a slot that an earlier sequence with rows has)
     const int32_t other = __builtin_amdgcn_readlane(q.slot, i), rows = __builtin_amdgcn_readlane(n, i);
     if (rows > 0 && n > 0 && (uint32_t)lane > i && q.slot == other && !wrong) { wrong = DE_BAD_SLOT; what = (uint32_t)q.slot; }
   }
@@ -53,6 +53,8 @@ __device__ __forceinline__ SeqLanes load_seqs(const RowSeqs& s, bool tell) {
   }
   return q;
 }
+
+__device__ __forceinline__ float uniform_f32(float v) { return __uint_as_float(uniform_u32(__float_as_uint(v))); }
 
 // The sequence that row r belongs to (the last that begins at or before it and has it), 64: none.
 __device__ __forceinline__ uint32_t seq_of_row(const SeqLanes& q, uint32_t r) {
@@ -73,7 +75,8 @@ __device__ __forceinline__ bool cache_row(const RowSeqs& s, uint32_t slot, uint3
 }
 
 // ------------------------------------------------------------------------------------ append
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16); }
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }   // to nearest even
 
 // 8 neighbouring elements as fp32
 template <typename T>
@@ -192,8 +195,9 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 // K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
-constexpr uint32_t kJoinWorkgroups = 2048;
 constexpr uint32_t kAttendMinBlocks = 2, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
+constexpr uint32_t kAttendWhole = 6;   // blocks that are not cut
+constexpr uint32_t kJoinWorkgroups = 1024;
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -202,41 +206,66 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t lds_u32 __attribute__((address_space(3)));
 
-// How a call's work is cut: every wavefront of both kernels works it out for itself from the lanes' sequences.
+// How a call's work is cut: every wavefront of both kernels works it out for itself from the lanes' sequences (a lane each, 16 at
+// most: one row of a data-parallel-primitive).
 struct Deal {
-  uint32_t tiles, chunks, blocks;   // of the lane's sequence: row tiles, runs of blocks a tile is cut into, blocks of a run
-  uint32_t first_unit;              // units of the sequences with more blocks, which come first
+  uint32_t tiles, chunks, blocks;   // of the lane's sequence: row tiles, runs of blocks that the longest is cut into, blocks of a run
+  uint32_t whole, units;            // runs that all tiles have; units, of one KV head
+  uint32_t first_unit;              // units of the sequences with more blocks, which come first (of all KV heads)
   uint32_t part;                    // floats of the workspace in front of the sequence's partial results
   uint32_t total;                   // units of all
 };
+template <typename T, class Op>
+__device__ __forceinline__ T row16_reduce(T v, Op op) {   // over the lane's row of 16
+  auto dpp = [](T x, auto ctrl) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+  v = op(v, dpp(v, std::integral_constant<int, 0xB1>{}));
+  v = op(v, dpp(v, std::integral_constant<int, 0x4E>{}));
+  v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));
+  return op(v, dpp(v, std::integral_constant<int, 0x140>{}));
+}
+// n / d for n below 2^24 (blocks of keys: max_seq is below 2^30).  The compiler's division, right for any number, is forty
+// operations, and there were six in front of a call's first load.
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d) {
+  uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
+  const int32_t r = (int32_t)(n - q * d);
+  return r < 0 ? q - 1u : (uint32_t)r >= d ? q + 1u : q;
+}
+// First of the tiles that have a run k (of `blocks` blocks), for a run that not all have: a tile's last row sees key k blocks 64.
+__device__ __forceinline__ uint32_t first_tile_of_run(uint32_t k, uint32_t blocks, uint32_t pos, uint32_t lg) {
+  return ((k * blocks * kBlockKeys - pos) << lg) / kTileRows;
+}
 template <int D>
 __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, uint32_t lg) {
   const uint32_t lane = threadIdx.x & 63u, T = (uint32_t)(q.end - q.begin), rows = T << lg;
+  auto add = [](auto x, auto y) { return x + y; };
   Deal d;
   d.tiles = (rows + kTileRows - 1u) / kTileRows;
   const uint32_t nb = T ? ((uint32_t)q.pos + T + kBlockKeys - 1u) / kBlockKeys : 0u;
-  uint64_t work = 0;
-  for (uint32_t i = 0; i < s.n_seqs; ++i)
-    work += (uint64_t)__builtin_amdgcn_readlane(d.tiles, i) *
-            (((uint32_t)__builtin_amdgcn_readlane(q.pos, i) + (uint32_t)__builtin_amdgcn_readlane(T, i) / 2u) / kBlockKeys + 1u);
-  uint32_t c = (uint32_t)max((uint64_t)kAttendMinBlocks, (work * s.n_kv + kAttendSlots - 1u) / kAttendSlots);
-  c = max(c, (s.max_seq + kBlockKeys * kAttendMostChunks - 1u) / (kBlockKeys * kAttendMostChunks));
-  for (;; c *= 2u) {   // (long enough that the partial results fit the workspace)
-    d.chunks = nb > c ? (nb + c - 1u) / c : 1u;
-    const float need = d.chunks > 1u ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(min(rows, kTileRows) * (D + 2u)) : 0.f;
-    float sum = 0.f;
-    for (uint32_t i = 0; i < s.n_seqs; ++i) sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(need), i));
-    if (sum <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u)) break;
+  const uint32_t few = row16_reduce(d.tiles, add) * s.n_kv;
+  const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
+  // few tiles: at most as many units as run at once, all about as long
+  uint32_t c = 1u + (uint32_t)(uniform_f32(work) / (float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots));
+  const uint32_t held = min(rows, kTileRows);
+  c = max(c, kAttendMinBlocks);
+  for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
+    d.chunks = nb > max(c, kAttendWhole) ? quotient(nb + c - 1u, c) : 1u;
+    const bool cut = T && d.chunks > 1u;
+    const float need = cut ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(held * (D + 2u)) : 0.f;
+    if (uniform_f32(row16_reduce(need, add)) <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u) && __all(d.chunks <= kAttendMostChunks)) break;
   }
-  d.blocks = (nb + d.chunks - 1u) / d.chunks;
-  if (!T) d.chunks = 0;
-  const uint32_t units = d.tiles * d.chunks * s.n_kv, floats = d.chunks > 1u ? units * min(rows, kTileRows) * (D + 2u) : 0u;
-  d.first_unit = d.part = d.total = 0;
+  d.blocks = max(1u, quotient(nb + d.chunks - 1u, d.chunks));
+  d.chunks = T ? quotient(nb + d.blocks - 1u, d.blocks) : 0u;
+  // a run whose first key lies behind the sequence's first new row is not every tile's
+  d.whole = T ? min(d.chunks, quotient((uint32_t)q.pos / kBlockKeys, d.blocks) + 1u) : 0u;
+  d.units = d.tiles * d.whole;
+  for (uint32_t k = d.whole; k < d.chunks; ++k) d.units += d.tiles - first_tile_of_run(k, d.blocks, (uint32_t)q.pos, lg);
+  const uint32_t units = d.units * s.n_kv, floats = d.chunks > 1u ? d.tiles * d.chunks * s.n_kv * held * (D + 2u) : 0u;
+  d.total = row16_reduce(units, add);
+  d.first_unit = d.part = 0;
   for (uint32_t i = 0; i < s.n_seqs; ++i) {
     const uint32_t onb = __builtin_amdgcn_readlane(nb, i), ou = __builtin_amdgcn_readlane(units, i), of = __builtin_amdgcn_readlane(floats, i);
     if (onb > nb || (onb == nb && i < lane)) d.first_unit += ou;
     if (i < lane) d.part += of;
-    d.total += ou;
   }
   return d;
 }
@@ -259,13 +288,20 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
 }
 
+// The largest of three, a NaN left out.  (fmaxf of results of a matrix instruction costs an operation more each, to quiet NaN.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 __device__ __forceinline__ uint32_t nonfinite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }   // bit 15 / 31: lower / upper
 
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) {
   constexpr uint32_t KS = D / 16, NT = D / 32, CPR = D / 8, RPI = 64 / CPR, IPW = 16 / RPI, ROWB = D * 2, TILE = kBlockKeys * ROWB;
   extern __shared__ __align__(16) unsigned char tiles_lds[];   // K, V of the even blocks, K, V of the odd ones, a flag
-  uint32_t& any_bad = *(uint32_t*)(tiles_lds + 4u * TILE);
+  uint32_t& flag = *(uint32_t*)(tiles_lds + 4u * TILE);
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), l31 = lane & 31u, half = lane >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
@@ -276,15 +312,25 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
 
   for (uint32_t u = blockIdx.x; u < total; u += gridDim.x) {
     // ---- the unit: sequence, tile of rows (the longest first), run of blocks, KV head (the one that neighbours in time share an L2 for)
-    const uint32_t mine = d.tiles * d.chunks * s.n_kv;
+    const uint32_t mine = d.units * s.n_kv;
     const uint32_t seq = (uint32_t)__builtin_ctzll(__ballot(mine && u >= d.first_unit && u < d.first_unit + mine));
     const uint32_t T = __builtin_amdgcn_readlane((uint32_t)(q.end - q.begin), seq), pos0 = __builtin_amdgcn_readlane(q.pos, seq);
     const uint32_t slot = __builtin_amdgcn_readlane(q.slot, seq), begin = __builtin_amdgcn_readlane(q.begin, seq);
     const uint32_t chunks = __builtin_amdgcn_readlane(d.chunks, seq), per = __builtin_amdgcn_readlane(d.blocks, seq);
-    const uint32_t v = u - __builtin_amdgcn_readlane(d.first_unit, seq), kvh = v % s.n_kv, w = v / s.n_kv;
-    const uint32_t chunk = w % chunks, tile = __builtin_amdgcn_readlane(d.tiles, seq) - 1u - w / chunks;
+    const uint32_t tiles = __builtin_amdgcn_readlane(d.tiles, seq), whole = __builtin_amdgcn_readlane(d.whole, seq);
+    const uint32_t v = u - __builtin_amdgcn_readlane(d.first_unit, seq), kvh = v % s.n_kv;
+    uint32_t w = v / s.n_kv, chunk = w / tiles;
+    if (chunk < whole) w -= chunk * tiles;
+    else {
+      w -= whole * tiles;
+      for (chunk = whole;; ++chunk) {
+        const uint32_t n = tiles - first_tile_of_run(chunk, per, pos0, lg);
+        if (w < n) break;
+        w -= n;
+      }
+    }
+    const uint32_t tile = tiles - 1u - w;
     const uint32_t nb = tile_blocks(pos0, T, tile, lg), b0 = chunk * per, b1 = min(nb, b0 + per);
-    if (b0 >= b1) continue;
     const uint32_t rows = T << lg, last = pos0 + T - 1u;   // the sequence's last row in the cache
     // ---- queries: B operand, lane = row, 8 columns a step and half
     const uint32_t r = tile * kTileRows + wave * 32u + l31, rr = min(r, rows - 1u), t = rr >> lg;
@@ -350,6 +396,14 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     float m = -3.402823466e38f, lsum = 0.f;   // of the lane's row (the sum: of the lane's keys)
     const uint32_t krow = l31 * ROWB, kx = (half ^ swizzle<D>(l31)) * 16u;
     const uint32_t rl = (lane & 15u) >> 2, un = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
+    uint32_t vat[NT][2];   // of the lane's 8 bytes of a step of 16 keys: columns 32 n .., keys 8 x + 4 half ..
+#pragma unroll
+    for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+      for (uint32_t x = 0; x < 2; ++x) {
+        const uint32_t place = ((n ^ (D == 128 ? rl : rl >> 1)) << 2) | (un ^ (half + 2u * x));
+        vat[n][x] = (8u * x + 4u * half + rl) * ROWB + place * 16u + 8u * (lane & 1u);
+      }
     drain_vmem();
     __syncthreads();
 
@@ -368,12 +422,12 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         uint32_t bad = 0;
 #pragma unroll
         for (uint32_t i = 0; i < TILE / 1024u; ++i) bad |= nonfinite(p[i]);
-        if (threadIdx.x == 0) any_bad = 0;
+        if (threadIdx.x == 0) flag = 0;
         __syncthreads();
-        if (bad) any_bad = 1;
+        if (bad) flag = 1;
         __syncthreads();
-        poisoned = any_bad != 0;
-        if (poisoned) {
+        poisoned = flag != 0;
+        if (__builtin_expect(poisoned, 0)) {
           for (uint32_t i = 0; i < TILE / 1024u; ++i) {
             const uint32_t x = p[i], n = nonfinite(x);
             p[i] = x & ~(((n & 0x8000u) ? 0xFFFFu : 0u) | ((n & 0x80000000u) ? 0xFFFF0000u : 0u));
@@ -382,6 +436,10 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         }
       }
       if (have && kv0 <= pos_hi) {
+        // A SIMD has a wavefront of each of two workgroups.  One that multiplies goes first, one that works out probabilities before
+        // one that requests or waits: the matrix pipe is fed while the other's vector operations fill its gaps (priorities all
+        // alike / as here: 4096 tokens 156 / 144 us, 2048 over 14000 976 / 915; multiplies alone preferred 153 / 969).
+        __builtin_amdgcn_s_setprio(2);
         f32x16 sc[2] = {f32x16{}, f32x16{}};
 #pragma unroll
         for (uint32_t k = 0; k < KS; ++k) {
@@ -391,19 +449,22 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
             sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), sc[n], 0, 0, 0);
           }
         }
+        __builtin_amdgcn_s_setprio(1);
         if (kv0 + kBlockKeys - 1u > pos_lo) {
+          const int32_t seen = (int32_t)(pos - kv0 - 4u * half);
 #pragma unroll
-          for (uint32_t n = 0; n < 2; ++n)
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (uint32_t i = 0; i < 16; ++i)
-              if (kv0 + 32u * n + 8u * (i >> 2) + 4u * half + (i & 3u) > pos) sc[n][i] = -INFINITY;
+            for (int i = 0; i < 16; ++i) sc[n][i] = 32 * n + 8 * (i >> 2) + (i & 3) > seen ? -INFINITY : sc[n][i];
         }
-        float mx = fmaxf(sc[0][0], sc[1][0]);
+        float mx = -INFINITY;
 #pragma unroll
-        for (uint32_t i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+        for (uint32_t i = 0; i < 16; ++i) mx = max3(mx, sc[0][i], sc[1][i]);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-        if (__any(mx > m)) {
+        // The reference m may stay behind the maximum by 2^8 (probabilities up to 256 lose nothing in bf16): with the exact one
+        // every other block of 32 rows has a row whose maximum grows, and rescales all outputs.
+        if (__any((mx - m) * scale2 > 8.f)) {
           const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f((m - mn) * scale2);
           lsum *= f;
           m = mn;
@@ -416,10 +477,14 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         for (uint32_t n = 0; n < 2; ++n)
 #pragma unroll
           for (uint32_t i = 0; i < 16; ++i) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][i], scale2, -ms));
-            lsum += p;
-            pf[2 * n + (i >> 3)][i & 7u] = (__bf16)p;
+            pf[2 * n + (i >> 3)][i & 7u] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[n][i], scale2, -ms));
           }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)   // the sum is of the rounded ones: the weights add up to one
+#pragma unroll
+          for (uint32_t i = 0; i < 8; i += 2)
+            lsum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[k][i], pf[k][i + 1]}, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
+        __builtin_amdgcn_s_setprio(2);
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k)
 #pragma unroll
@@ -427,13 +492,12 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
             union { s16x4 h[2]; bf16x8 v; } vf;
 #pragma unroll
             for (uint32_t x = 0; x < 2; ++x) {
-              const uint32_t place = D == 128 ? ((n ^ rl) << 2) | (un ^ (half + 2u * x)) : ((n ^ (rl >> 1)) << 2) | (un ^ (half + 2u * x));
-              const uint32_t at = vt + (16u * k + 8u * x + 4u * half + rl) * ROWB + place * 16u + 8u * (lane & 1u);
-              vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
+              vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(vt + vat[n][x]) + 16u * k * ROWB / 8u);
             }
             o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[k], o[n], 0, 0, 0);
           }
-        if (poisoned) {
+        __builtin_amdgcn_s_setprio(0);
+        if (__builtin_expect(poisoned, 0)) {
           for (uint32_t j = 0; j < kBlockKeys && kv0 + j <= pos_hi; ++j) {
             size_t at = 0;
             if (!cache_row(s, slot, kvh, kv0 + j, &at) || kv0 + j > pos) continue;
@@ -456,17 +520,18 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     if (r < rows) {
       if (nb <= per) {
         const float inv = 1.0f / l;
-        uint16_t* to = a.out + (size_t)(begin + t) * a.out_stride + (size_t)head * D + 4u * half;
+        uint16_t* to = a.out + (size_t)(begin + t) * a.out_stride + (size_t)head * D + 8u * half;
 #pragma unroll
         for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
-          for (uint32_t i = 0; i < 4; ++i) {
-            const u32x2 x = {pack_bf16(o[n][4 * i] * inv, o[n][4 * i + 1] * inv), pack_bf16(o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv)};
-            *as_global((u32x2*)(to + 32u * n + 8u * i)) = x;
+          for (uint32_t i = 0; i < 16; i += 8) {   // a lane has 4 of 8 columns, the other half's lane the others: 8 of one lane, 8 of the other
+            const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(o[n][i] * inv, o[n][i + 1] * inv), pack_bf16(o[n][i + 4] * inv, o[n][i + 5] * inv), false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16(o[n][i + 2] * inv, o[n][i + 3] * inv), pack_bf16(o[n][i + 6] * inv, o[n][i + 7] * inv), false, false);
+            *as_global((u32x4*)(to + 32u * n + 2u * i)) = u32x4{x[0], y[0], x[1], y[1]};
           }
       } else {
         const uint32_t held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
-        float* part = (float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)v * held * (D + 2u);
+        float* part = (float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)((tile * chunks + chunk) * s.n_kv + kvh) * held * (D + 2u);
         float* to = part + (size_t)in_tile * D + 4u * half;
 #pragma unroll
         for (uint32_t n = 0; n < NT; ++n)
@@ -481,6 +546,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
 // Joins the partial results of a row whose tile was cut into runs, in their order: a wavefront per row and query head.
 template <int D>
 __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uint32_t lg) {
+  __shared__ float weight[4][kAttendMostChunks + 16u];
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
   const SeqLanes q = load_seqs(s, false);
@@ -496,53 +562,43 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
   const uint32_t n = (tile_blocks(pos0, T, tile, lg) + per - 1u) / per;
   if (n <= 1u) continue;
   const uint32_t rows = T << lg, held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
-  const uint32_t v0 = (__builtin_amdgcn_readlane(d.tiles, seq) - 1u - tile) * chunks * s.n_kv + (head >> lg);
+  const uint32_t v0 = tile * chunks * s.n_kv + (head >> lg);
   const size_t stride = (size_t)s.n_kv * held * (D + 2u);
   const float* part = (const float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)v0 * held * (D + 2u);
-  // a lane holds maximum and sum of the runs lane, lane + 64, ..; then all loads of a stretch of runs are in flight at once
-  float m[kAttendMostChunks / 64], w[kAttendMostChunks / 64], M = -INFINITY, l = 0.f, o[D / 64] = {};
+  // the runs' weights, a lane a run (and the 64th, .. after it), into LDS; then the loads of 16 runs are in flight at once
+  float M = -INFINITY, l = 0.f, o[D / 64] = {};
+  f32x2 ml[kAttendMostChunks / 64];
 #pragma unroll
   for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
-    m[i] = -INFINITY;
-    w[i] = 0.f;
-    if (64u * i + lane < n) {
-      const f32x2 ml = *as_global((const f32x2*)(part + (64u * i + lane) * stride + (size_t)held * D + 2u * in_tile));
-      m[i] = ml.x;
-      w[i] = ml.y;
-    }
-    M = fmaxf(M, m[i]);
+    ml[i] = f32x2{-INFINITY, 0.f};
+    if (64u * i + lane < n) ml[i] = *as_global((const f32x2*)(part + (64u * i + lane) * stride + (size_t)held * D + 2u * in_tile));
   }
+#pragma unroll
+  for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) M = fmaxf(M, ml[i].x);
   M = wave_max_dpp(M);
 #pragma unroll
   for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
-    const float f = __builtin_amdgcn_exp2f(m[i] - M);
-    l = fmaf(w[i], f, l);
-    w[i] = f;
+    const float f = __builtin_amdgcn_exp2f(ml[i].x - M);
+    l = fmaf(ml[i].y, f, l);
+    weight[wave][64u * i + lane] = f;
   }
   l = wave_sum_dpp(l);
   const float* p = part + (size_t)in_tile * D + (D / 64) * lane;
+  for (uint32_t c = 0; c < n; c += 16u) {
+    float v[16][D / 64];
 #pragma unroll
-  for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
-    if (64u * i >= n) break;
-    const uint32_t here = min(64u, n - 64u * i);
-    for (uint32_t c = 0; c < here; c += 8u) {
-      float v[8][D / 64];
+    for (uint32_t j = 0; j < 16; ++j)
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j)
+      for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(c + j, n - 1u) * stride + e];
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(64u * i + c + j, n - 1u) * stride + e];
+    for (uint32_t j = 0; j < 16; ++j)
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
-        const float f = c + j < here ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[i]), (c + j) & 63u)) : 0.f;
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) o[e] = c + j < here ? fmaf(v[j][e], f, o[e]) : o[e];
-      }
-    }
+      for (int e = 0; e < D / 64; ++e) o[e] = c + j < n ? fmaf(v[j][e], weight[wave][c + j], o[e]) : o[e];
   }
   const float inv = 1.0f / l;
   uint16_t* to = a.out + (size_t)row * a.out_stride + (size_t)head * D + (D / 64) * lane;
   if constexpr (D == 128) *as_global((uint32_t*)to) = pack_bf16(o[0] * inv, o[1] * inv);
-  else *as_global(to) = f32_to_bf16(o[0] * inv);
+  else *as_global(to) = (uint16_t)pack_bf16(o[0] * inv, 0.f);
   }
 }
 
@@ -556,10 +612,13 @@ hipError_t rows_prepare() {
 
 template <int D, bool PAGED>
 static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t stream) {
+  // units: one per tile, and up to kAttendSlots more where tiles are cut (a workgroup without one has worked that out for nothing;
+  // one takes several where there are more)
   const uint64_t tiles = (((uint64_t)a.s.n_rows << lg) / kTileRows + a.s.n_seqs) * a.s.n_kv;
-  rows_attend_kernel<D, PAGED><<<dim3((uint32_t)std::min<uint64_t>(tiles + 2u * kAttendSlots, 1u << 20)), dim3(256), attend_lds(D), stream>>>(a, lg);
+  const uint32_t grid = tiles <= kAttendSlots / 2u ? kAttendSlots : (uint32_t)std::min<uint64_t>(tiles + kAttendSlots / 4u, 1u << 20);
+  rows_attend_kernel<D, PAGED><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.s.max_seq <= kAttendWhole * kBlockKeys) return e;
   rows_attend_join_kernel<D><<<dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
   return hipGetLastError();
 }
@@ -575,11 +634,13 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 //   s = sum e^(x - m) without one of the largest, t = sum e^(x - m) (x - m)
 // (ln p = x - m - log1p(s): nothing is lost of a token that is all but certain; entropy = log1p(s) - t / (1 + s)), and its
 // best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
-// With few rows a row is cut into runs of steps, one a workgroup, and a second kernel joins these.
+// With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
 constexpr uint32_t kStep = 1024;          // logits of a wavefront's step
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
 constexpr uint32_t kLogprobWorkgroups = 1024;   // that a call is cut into where its rows are fewer
 constexpr uint32_t kLogprobManyRows = 2048;     // a wavefront a row from here on
+static_assert(kLogprobManyRows <= kRowsArrivals, "a counter a row that is cut");
+constexpr uint32_t kNotLast = 0xFFFFFFFFu;
 
 // A logit and its token as one number: larger logits first, of equal ones the lower token.  0: none.
 __device__ __forceinline__ uint64_t entry_of(float x, uint32_t token) {
@@ -615,22 +676,46 @@ __device__ __forceinline__ RowSum join_sums(const RowSum& a, uint32_t n) {
   return RowSum{m, wave_sum_dpp(s), wave_sum_dpp(t)};
 }
 
-// The best k of n entries in LDS, in order, into best [k] (empty before).  The whole workgroup calls it.
+// The best k of n entries in LDS, in order, into best [k] (empty before).  The whole workgroup calls it: an entry's place is the
+// number of entries above it, eight lanes count an eighth of them each.
 __device__ __forceinline__ void rank_entries(const uint64_t* list, uint32_t n, uint32_t k, uint64_t* best) {
-  for (uint32_t i = threadIdx.x; i < n; i += 256u) {
-    const uint64_t mine = list[i];
+  for (uint32_t i0 = 0; i0 < n; i0 += 32u) {
+    const uint32_t i = i0 + (threadIdx.x >> 3);
+    const uint64_t mine = i < n ? list[i] : 0;
     uint32_t rank = 0;
-#pragma unroll 8
-    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine;
-    if (mine && rank < k) best[rank] = mine;
+#pragma unroll 2
+    for (uint32_t j = threadIdx.x & 7u; j < n; j += 8u) rank += list[j] > mine;
+    rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0xB1, 0xF, 0xF, true);    // lane ^ 1
+    rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0x4E, 0xF, 0xF, true);    // lane ^ 2
+    rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0x141, 0xF, 0xF, true);   // mirror of 8
+    if (mine && rank < k && (threadIdx.x & 7u) == 0) best[rank] = mine;
   }
+}
+// A lower bound, its upper 16 bits, of the n-th largest of the lanes' numbers (0 where fewer have any).
+__device__ __forceinline__ uint32_t nth_largest(uint32_t key, uint32_t n) {
+  uint32_t p = 0;
+#pragma unroll 1
+  for (uint32_t bit = 0x40000000u; bit > 0x8000u; bit >>= 2) {   // two bits a time: three counts that do not wait for each other
+    const uint32_t a = (uint32_t)__popcll(__ballot(key >= (p | bit))), b = (uint32_t)__popcll(__ballot(key >= (p | 2u * bit))),
+                   c = (uint32_t)__popcll(__ballot(key >= (p | 3u * bit)));
+    p |= c >= n ? 3u * bit : b >= n ? 2u * bit : a >= n ? bit : 0u;
+  }
+  return p;
+}
+
+// ln(1 + s), s >= 0, in a few operations: 2 artanh(s / (2 + s)) as a series below one (the rest of it is under 2e-8 of the
+// value), the logarithm above.
+__device__ __forceinline__ float log1p_fast(float s) {
+  const float z = s / (2.f + s), y = z * z;
+  const float p = fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(y, 1.f / 15, 1.f / 13), y, 1.f / 11), y, 1.f / 9), y, 1.f / 7), y, 1.f / 5), y, 1.f / 3), y, 1.f);
+  return s < 1.f ? 2.f * z * p : __logf(1.f + s);
 }
 
 // What is written for a row, by one wavefront: `mine` is lane j's j-th best entry, empty ones last.
 __device__ __forceinline__ void write_row(const LogprobArgs& a, uint32_t row, const RowSum& r, float asked, uint64_t mine) {
   const uint32_t lane = threadIdx.x & 63u;
   const bool none = !(r.m > -INFINITY) || r.m == INFINITY || r.s != r.s;
-  const float norm = log1pf(r.s), nan = __uint_as_float(0x7FC00000u);
+  const float norm = log1p_fast(r.s), nan = __uint_as_float(0x7FC00000u);
   if (lane == 0) {
     if (a.entropy) as_global(a.entropy)[row] = none ? nan : norm - r.t / (1.f + r.s);
     if (a.tokens) {
@@ -672,7 +757,7 @@ __device__ __forceinline__ float asked_logit(const LogprobArgs& a, uint32_t row)
   return t >= 0 && (uint32_t)t < a.vocab ? logit_at((const T*)a.logits + (size_t)row * a.stride, (size_t)t) : 0.f;
 }
 
-// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [128]) and
+// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [192]) and
 // joined with them 64 at a time: an entry's place is the number of entries above it.  (Put in place one by one, the lanes
 // behind shifted, a row of 151936 with 20 alternatives took 18.8 us instead of 8.7, 4096 rows of 32000 with 4 106 instead of 94.)
 struct Best {
@@ -684,12 +769,14 @@ struct Best {
       const uint32_t n = min(64u, waiting - at);
       const uint64_t now = lane < n ? fresh[at + lane] : 0;
       uint32_t place_now = 0, place_old = lane;
+#pragma unroll 2
       for (uint32_t i = 0; i < n; ++i) {
-        const uint64_t e = readlane64(now, i);
+        const uint64_t e = fresh[at + i];
         place_now += e > now;
         place_old += e > mine;
       }
-      for (uint32_t i = 0; i < count; ++i) place_now += readlane64(mine, i) > now;
+#pragma unroll 2
+      for (uint32_t i = 0; i < count; ++i) place_now += sorted[i] > now;
       if (lane < n && place_now < n_top) sorted[place_now] = now;
       if (lane < count && place_old < n_top) sorted[place_old] = mine;
       count = min(n_top, count + n);
@@ -700,13 +787,70 @@ struct Best {
   }
 };
 
+// The workgroup's run of a row (sums r and the lanes' best entries, in wavefront 0) to the device's coherence point; the
+// workgroup that arrives last at the row's counter, and it alone, goes on with all of them: true, r and `mine` the row's.
+__device__ __forceinline__ bool join_runs(const LogprobArgs& a, uint32_t row, uint32_t chunk, uint32_t chunks, RowSum& r, uint64_t& mine, uint64_t* lds) {
+  uint64_t *best = lds, &least = lds[MPK_ROWS_MAX_TOP], *list = lds + MPK_ROWS_MAX_TOP + 2;   // list: [chunks * k]
+  uint32_t& n = (uint32_t&)lds[MPK_ROWS_MAX_TOP + 1];
+  const uint32_t lane = threadIdx.x & 63u, k = a.n_top;
+  uint64_t *sums = (uint64_t*)a.work + (size_t)row * chunks * (2u + k), *entries = sums + 2u * chunks;   // [chunks][2], [chunks][k]
+  if (threadIdx.x < 64u) {
+    if (lane == 0) { st_act2((float*)(sums + 2u * chunk), r.m, r.s); st_act((float*)(sums + 2u * chunk + 1u), r.t); }
+    if (lane < k) __hip_atomic_store(as_global(entries + chunk * k + lane), mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    drain_vmem();
+    if (lane == 0) {
+      uint32_t* arrived = a.arrivals + (size_t)row * kArrivalStride;
+      const bool last = __hip_atomic_fetch_add(as_global(arrived), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == chunks;
+      if (last) st_act_u32(arrived, 0u);   // as the next call finds it
+      n = last ? 0u : kNotLast;
+    }
+  }
+  __syncthreads();
+  if (n == kNotLast) return false;
+  // everything that the runs left, in one round of loads
+  constexpr uint32_t kPer = kLogprobChunks * MPK_ROWS_MAX_TOP / 256u;
+  uint64_t e[kPer], nth_best = 0;
+  const uint32_t nth = min(k, (2u * k + chunks - 1u) / chunks);
+#pragma unroll
+  for (uint32_t j = 0; j < kPer; ++j) e[j] = threadIdx.x + 256u * j < chunks * k ? ld_relaxed64(entries + threadIdx.x + 256u * j) : 0;
+  if (threadIdx.x < 64u) {
+    r = RowSum{-INFINITY, 0.f, 0.f};
+    if (lane < chunks) {
+      if (k) nth_best = ld_relaxed64(entries + lane * k + nth - 1u);
+      const float2 ms = ld_act2((const float*)(sums + 2u * lane));
+      r.m = ms.x; r.s = ms.y; r.t = ld_act((const float*)(sums + 2u * lane + 1u));
+    }
+    r = join_sums(r, chunks);
+    // ceil(k / nth) runs have nth entries at or above the one that this many runs' nth entries are not below: k of the row are,
+    // and few others where about half of the runs have one
+    if (k) {
+      const uint32_t p = nth_largest((uint32_t)(nth_best >> 32), (k + nth - 1u) / nth);
+      if (lane == 0) least = (uint64_t)p << 32;
+      if (lane < k) best[lane] = 0;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t j = 0; j < kPer; ++j)
+    if (256u * j < chunks * k && e[j] && e[j] >= least) list[atomicAdd(&n, 1u)] = e[j];   // (in any order: an entry's rank goes by all of them)
+  __syncthreads();
+  rank_entries(list, n, k, best);
+  __syncthreads();
+  mine = lane < k ? best[lane] : 0;
+  return true;
+}
+
 // W wavefronts of a workgroup share a run (4, or 1: a run each).
 template <typename T, uint32_t W>
 __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t steps) {
   constexpr uint32_t E = 16 / sizeof(T), V = 16 / E;   // logits of 16 bytes, such loads of a step
-  __shared__ uint64_t fresh[4][128], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
-  __shared__ __align__(16) float offered[4][64][20];   // (20: reads of 16 logits of four lanes spread over the banks)
+  __shared__ uint64_t fresh[4][192], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
+  // what hot steps pass from lane to lane (20: reads of 16 logits of four lanes spread over the banks), then the entries of the join
+  __shared__ __align__(16) uint64_t lists[4 * 64 * 20 / 2];
+  float(*offered)[64][20] = (float(*)[64][20])lists;
+  static_assert(sizeof(lists) >= (kLogprobChunks * MPK_ROWS_MAX_TOP + MPK_ROWS_MAX_TOP + 2) * 8, "entries of all runs");
   __shared__ RowSum sums[4];
+  __shared__ uint32_t bounds[4];
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), part_of = W == 1 ? 0u : wave;
   const uint32_t unit = W == 1 ? blockIdx.x * 4u + wave : blockIdx.x, row = unit / chunks, chunk = unit - row * chunks, k = a.n_top;
   if (W == 1 && row >= a.n_rows) return;
@@ -719,7 +863,7 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
 
   RowSum r = {-INFINITY, 0.f, 0.f};
   Best best;
-  float limit = -INFINITY;   // the last of the best (nothing to beat without alternatives but the largest)
+  float bound = -INFINITY, limit = -INFINITY;   // the row's alternatives are not below the first; the last of the best (nothing to beat without alternatives but the largest)
   u32x4 next[V];
   auto request = [&](uint32_t first) {
 #pragma unroll
@@ -727,9 +871,9 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   };
   uint32_t at = v0 + part_of * (kStep / E);
   if (at < v1) request(at);
-  if (chunks == 1u && part_of == 0) asked = asked_logit<T>(a, row);
+  if (part_of == 0) asked = asked_logit<T>(a, row);
   // The row's edges, what lies in front of the first and behind the last load of 16 bytes, come last, as one step.
-  bool edges = false;
+  bool edges = false, start = W > 1;
   for (;;) {
     float y[16];
     const uint32_t first = at;
@@ -752,17 +896,35 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
           if (first + (j / E) * 64u + lane >= v1) y[j] = -INFINITY;
       }
     } else {
-      if (edges || chunk || part_of || !(head + tail)) break;
-      edges = true;
 #pragma unroll
       for (int j = 0; j < 16; ++j) y[j] = -INFINITY;
-      if (lane < head + tail) y[0] = logit_at(x, lane < head ? lane : a.vocab - tail + (lane - head));
+      if (!start) {
+        if (edges || chunk || part_of || !(head + tail)) break;
+        edges = true;
+      }
+      if (edges && lane < head + tail) y[0] = logit_at(x, lane < head ? lane : a.vocab - tail + (lane - head));
     }
     float mx = y[0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) mx = fmaxf(mx, y[j]);
-    // (tokens ascend, so an equal logit does not beat one; the edges come out of order)
-    uint64_t hot = __ballot(mx > limit || (edges && mx == limit));
+    float least = -3.402823466e38f;
+    const bool equals = edges || start;   // (tokens ascend, so an equal logit does not beat one; the edges come out of order, the bound is a logit)
+    if (start) {
+      // Every wavefront's first step together: a quarter of the alternatives lie at or above a wavefront's bound, all of them
+      // above the least bound, and what a wavefront gathers is a quarter, too.
+      start = false;
+      if (k) {
+        const uint32_t p = nth_largest(mx == mx ? (uint32_t)(entry_of(mx, 0) >> 32) : 0u, (k + W - 1u) / W);
+        if (lane == 0) bounds[wave] = p;
+        __syncthreads();
+        const uint32_t all = min(min(bounds[0], bounds[1]), min(bounds[2], bounds[3]));
+        if (all > 0x007FFFFFu) {
+          least = fmaxf(least, entry_logit((uint64_t)all << 32));
+          limit = bound = least;
+        }
+      }
+    }
+    uint64_t hot = __ballot(mx > limit || (equals && mx == limit));
     if (hot) {
       const float m = wave_max_dpp(mx);
       const bool more = m > r.m;
@@ -776,13 +938,9 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
         r.m = m;
       }
       if (k) {
-        float least = -3.402823466e38f;
         if ((uint32_t)__popcll(hot) > k) {
           // more lanes than places: k logits are at or above the k-th largest of the lanes' largest (its upper 16 bits)
-          const uint32_t key = mx == mx ? (uint32_t)(entry_of(mx, 0) >> 32) : 0u;
-          uint32_t p = 0;
-          for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
-            if ((uint32_t)__popcll(__ballot(key >= (p | bit))) >= k) p |= bit;
+          const uint32_t p = nth_largest(mx == mx ? (uint32_t)(entry_of(mx, 0) >> 32) : 0u, k);
           if (p > 0x007FFFFFu) least = fmaxf(least, entry_logit((uint64_t)p << 32));
           hot = __ballot(mx >= least);
         }
@@ -790,24 +948,28 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
 #pragma unroll
           for (int j = 0; j < 16; j += 4) *(float4*)&offered[wave][lane][j] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
         }
-        while (hot) {   // four such lanes at a time
-          uint32_t from = 64u;
+        while (hot) {   // eight such lanes at a time
+          uint32_t from[2] = {64u, 64u};
 #pragma unroll
-          for (uint32_t g = 0; g < 4; ++g) {
-            if (hot && lane >> 4 == g) from = (uint32_t)__builtin_ctzll(hot);
+          for (uint32_t g = 0; g < 8; ++g) {
+            if (hot && lane >> 4 == (g & 3u)) from[g >> 2] = (uint32_t)__builtin_ctzll(hot);
             hot &= hot - 1ull;
           }
           const uint32_t j = lane & 15u;
-          const float v = from < 64u ? offered[wave][from & 63u][j] : -INFINITY;
-          const uint32_t token = edges ? (from < head ? from : a.vocab - tail + (from - head)) : head + (first + (j / E) * 64u + from) * E + j % E;
-          const uint64_t e = entry_of(v, token), b = __ballot(v >= least && e > best.last);
-          if (!b) continue;
-          if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
-          best.waiting += (uint32_t)__popcll(b);
-          if (best.waiting >= 64u) best.join(fresh[wave], sorted[wave], k);
+          float v[2];
+#pragma unroll
+          for (uint32_t g = 0; g < 2; ++g) v[g] = offered[wave][from[g] & 63u][j];
+#pragma unroll
+          for (uint32_t g = 0; g < 2; ++g) {
+            const uint32_t l = from[g], token = edges ? (l < head ? l : a.vocab - tail + (l - head)) : head + (first + (j / E) * 64u + l) * E + j % E;
+            const uint64_t e = entry_of(v[g], token), b = __ballot(l < 64u && v[g] >= least && e > best.last);
+            if (!b) continue;
+            if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
+            best.waiting += (uint32_t)__popcll(b);
+          }
+          if (best.waiting >= 64u || !hot) best.join(fresh[wave], sorted[wave], k);
         }
-        if (best.waiting) best.join(fresh[wave], sorted[wave], k);
-        limit = best.last ? entry_logit(best.last) : -INFINITY;
+        limit = fmaxf(bound, best.last ? entry_logit(best.last) : -INFINITY);
       } else limit = r.m;
       if (more) {   // one of the largest stays out of the sum
         bool out = lane == (uint32_t)__builtin_ctzll(__ballot(mx == m));
@@ -843,56 +1005,12 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
       rank_entries(list, 4u * k, k, first_best);
       __syncthreads();
     }
-    if (wave) return;
     r = join_sums(sums[lane & 3u], 4);
     if (lane < k) mine = first_best[lane];
+    if (chunks > 1u && !join_runs(a, row, chunk, chunks, r, mine, lists)) return;
+    if (wave) return;
   }
-  if (chunks == 1u) { write_row(a, row, r, asked, mine); return; }
-  uint64_t* part = (uint64_t*)a.work + (size_t)unit * (2u + k);
-  if (lane == 0) { as_global((float*)part)[0] = r.m; as_global((float*)part)[1] = r.s; as_global((float*)part)[2] = r.t; }
-  if (lane < k) as_global(part)[2 + lane] = mine;
-}
-
-// Joins the runs of a row: a workgroup each.
-template <typename T>
-__global__ void __launch_bounds__(256) rows_logprobs_join_kernel(LogprobArgs a, uint32_t chunks) {
-  __shared__ uint64_t list[kLogprobChunks * MPK_ROWS_MAX_TOP], best[MPK_ROWS_MAX_TOP], least;
-  __shared__ uint32_t n;
-  const uint32_t lane = threadIdx.x & 63u, row = blockIdx.x, k = a.n_top, size = 2u + k;
-  const uint64_t* part = (const uint64_t*)a.work + (size_t)row * chunks * size;
-  RowSum r = {-INFINITY, 0.f, 0.f};
-  float asked = 0.f;
-  if (threadIdx.x < 64u) {
-    if (k) {
-      // ceil(k / nth) runs have nth entries at or above the one that this many runs' nth entries are not below: k of the row
-      // are, and few others where about half of the runs have one
-      const uint32_t nth = min(k, (2u * k + chunks - 1u) / chunks), at = (k + nth - 1u) / nth;
-      const uint64_t mine = lane < chunks ? as_global(part)[lane * size + 1u + nth] : 0;
-      uint32_t above = 0;
-      for (uint32_t i = 0; i < chunks; ++i) above += readlane64(mine, i) > mine;
-      const uint64_t holds = __ballot(mine && above == at - 1u);
-      if (lane == 0) { least = 0; n = 0; }
-      if (holds && lane == (uint32_t)__builtin_ctzll(holds)) least = mine;
-      if (lane < k) best[lane] = 0;
-    }
-    asked = asked_logit<T>(a, row);
-    if (lane < chunks) {
-      const MPK_GLOBAL float* p = (const MPK_GLOBAL float*)(part + lane * size);
-      r.m = p[0]; r.s = p[1]; r.t = p[2];
-    }
-  }
-  if (k) {
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < chunks * k; i += 256u) {
-      const uint32_t c = i / k;
-      const uint64_t e = as_global(part)[c * size + 2u + (i - c * k)];
-      if (e && e >= least) list[atomicAdd(&n, 1u)] = e;   // (in any order: an entry's rank goes by all of them)
-    }
-    __syncthreads();
-    rank_entries(list, n, k, best);
-    __syncthreads();
-  }
-  if (threadIdx.x < 64u) write_row(a, row, join_sums(r, chunks), asked, lane < k ? best[lane] : 0);
+  write_row(a, row, r, asked, mine);
 }
 
 template <typename T>
@@ -905,9 +1023,6 @@ static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   const uint32_t all = std::max(1u, (a.vocab + 4u * kStep - 1u) / (4u * kStep)), want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
   const uint32_t n = std::min(std::min(want, all), kLogprobChunks), steps = 4u * ((all + n - 1u) / n), chunks = (4u * all + steps - 1u) / steps;
   rows_logprobs_kernel<T, 4><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, steps);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || chunks == 1u) return e;
-  rows_logprobs_join_kernel<T><<<dim3(a.n_rows), dim3(256), 0, stream>>>(a, chunks);
   return hipGetLastError();
 }
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream) {

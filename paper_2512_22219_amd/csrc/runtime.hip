@@ -132,6 +132,7 @@ struct mpk_graph {
   struct mpk_server* server = nullptr;        // serving graph: the server attached to it
   // what the calls on rows (mpk_rows_*) need of the model
   uint16_t *cache_k = nullptr, *cache_v = nullptr;
+  uint32_t* d_arrivals = nullptr;
   std::vector<std::pair<const uint16_t*, const uint16_t*>> qk_gains;   // per layer: q_norm, k_norm (null without the norm)
 };
 
@@ -429,6 +430,7 @@ extern "C" mpk_status mpk_compile(const mpk_model_config* cfg, const mpk_weight_
   ZeroBlock control;
   control.add(&g->d_counters, h.events.size());
   control.add(&g->d_err, 8);
+  control.add(&g->d_arrivals, kRowsArrivals * kArrivalStride);
   control.add(&g->d_grp, h.n_group_counters);
   control.add(&g->d_hier, (size_t)std::max(h.n_hier_events, 1u) * kHierWordsPerEvent);
   if (o.debug_flags & MPK_DEBUG_TRACE) control.add(&g->d_trace, h.tasks.size() * kTraceSlots);
@@ -720,6 +722,7 @@ extern "C" mpk_status mpk_graph_reset(mpk_graph* g) {
   HIP_TRY(hipDeviceSynchronize());
   HIP_TRY(hipMemset(g->d_counters, 0, g->h.events.size() * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_err, 0, 8 * sizeof(uint32_t)));
+  HIP_TRY(hipMemset(g->d_arrivals, 0, kRowsArrivals * kArrivalStride * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_hier, 0, (size_t)std::max(g->h.n_hier_events, 1u) * kHierWordsPerEvent * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_grp, 0, std::max<size_t>(g->h.n_group_counters, 1) * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_rope, 0xFF, g->rope_words * sizeof(float)));
@@ -1150,6 +1153,7 @@ static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs,
   s->n_q = h.cfg.n_q_heads; s->n_kv = h.cfg.n_kv_heads; s->head_dim = h.cfg.head_dim;
   s->batch = h.cfg.batch; s->max_seq = h.cfg.max_seq;
   s->err = g->d_err;
+  s->arrivals = g->d_arrivals;
   size_t rows = (size_t)(h.opt.kv_batch ? h.opt.kv_batch : h.cfg.batch) * h.cfg.max_seq;   // of one layer and KV head
   if (h.opt.kv_page_size) {
     s->table = g->page_table;
@@ -1227,7 +1231,7 @@ extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const voi
   a.tokens = tokens; a.logprobs = logprobs; a.entropy = entropy;
   a.top_tokens = top_tokens; a.top_logprobs = top_logprobs;
   a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
-  a.work = workspace; a.err = g->d_err;
+  a.work = workspace; a.err = g->d_err; a.arrivals = g->d_arrivals;
   HIP_TRY(launch_rows_logprobs(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
   return MPK_OK;
 }
