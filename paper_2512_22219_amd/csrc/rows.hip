@@ -198,6 +198,7 @@ constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 2, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendWhole = 6;   // blocks that are not cut
 constexpr uint32_t kJoinWorkgroups = 1024;
+constexpr uint32_t kAttendHeader = 1024;   // floats of the workspace in front of the partial results
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -206,12 +207,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t lds_u32 __attribute__((address_space(3)));
 
-// How a call's work is cut: every wavefront of both kernels works it out for itself from the lanes' sequences (a lane each, 16 at
-// most: one row of a data-parallel-primitive).
+// How a call's work is cut: every wavefront works it out for itself from the lanes' sequences (a lane each, 16 at most: one row
+// of a data-parallel-primitive).
 struct Deal {
   uint32_t tiles, chunks, blocks;   // of the lane's sequence: row tiles, runs of blocks that the longest is cut into, blocks of a run
   uint32_t whole, units;            // runs that all tiles have; units, of one KV head
-  uint32_t first_unit;              // units of the sequences with more blocks, which come first (of all KV heads)
+  uint32_t first_unit;              // units in front of the sequence's (of all KV heads)
   uint32_t part;                    // floats of the workspace in front of the sequence's partial results
   uint32_t total;                   // units of all
 };
@@ -222,6 +223,16 @@ __device__ __forceinline__ T row16_reduce(T v, Op op) {   // over the lane's row
   v = op(v, dpp(v, std::integral_constant<int, 0x4E>{}));
   v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));
   return op(v, dpp(v, std::integral_constant<int, 0x140>{}));
+}
+// Sum over the lanes in front, in the lane's row of 16.
+__device__ __forceinline__ uint32_t row16_before(uint32_t v) {
+  uint32_t x = v;
+  auto add = [&](auto ctrl) { x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true); };
+  add(std::integral_constant<int, 0x111>{});   // row_shr 1, 2, 4, 8
+  add(std::integral_constant<int, 0x112>{});
+  add(std::integral_constant<int, 0x114>{});
+  add(std::integral_constant<int, 0x118>{});
+  return x - v;
 }
 // n / d for n below 2^24 (blocks of keys: max_seq is below 2^30).  The compiler's division, right for any number, is forty
 // operations, and there were six in front of a call's first load.
@@ -244,7 +255,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   const uint32_t few = row16_reduce(d.tiles, add) * s.n_kv;
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
   // few tiles: at most as many units as run at once, all about as long
-  uint32_t c = 1u + (uint32_t)(uniform_f32(work) / (float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots));
+  uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots)));
   const uint32_t held = min(rows, kTileRows);
   c = max(c, kAttendMinBlocks);
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
@@ -261,11 +272,14 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   for (uint32_t k = d.whole; k < d.chunks; ++k) d.units += d.tiles - first_tile_of_run(k, d.blocks, (uint32_t)q.pos, lg);
   const uint32_t units = d.units * s.n_kv, floats = d.chunks > 1u ? d.tiles * d.chunks * s.n_kv * held * (D + 2u) : 0u;
   d.total = row16_reduce(units, add);
-  d.first_unit = d.part = 0;
-  for (uint32_t i = 0; i < s.n_seqs; ++i) {
-    const uint32_t onb = __builtin_amdgcn_readlane(nb, i), ou = __builtin_amdgcn_readlane(units, i), of = __builtin_amdgcn_readlane(floats, i);
-    if (onb > nb || (onb == nb && i < lane)) d.first_unit += ou;
-    if (i < lane) d.part += of;
+  d.part = row16_before(floats);
+  d.first_unit = row16_before(units);
+  if (uniform_u32(d.total) > kAttendSlots) {   // not all at once: the sequences with more blocks first
+    d.first_unit = 0;
+    for (uint32_t i = 0; i < s.n_seqs; ++i) {
+      const uint32_t onb = __builtin_amdgcn_readlane(nb, i), ou = __builtin_amdgcn_readlane(units, i);
+      if (onb > nb || (onb == nb && i < lane)) d.first_unit += ou;
+    }
   }
   return d;
 }
@@ -308,6 +322,11 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
   const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
   const Deal d = deal_units<D>(s, q, lg);
   const uint32_t total = uniform_u32(d.total);
+  if (blockIdx.x == 0 && threadIdx.x < kMaxRowSeqs) {   // what the join needs of it
+    MPK_GLOBAL u32x4* to = as_global((u32x4*)a.work) + 2u * threadIdx.x;
+    to[0] = u32x4{(uint32_t)q.begin, (uint32_t)q.end, (uint32_t)q.pos, d.chunks};
+    to[1] = u32x4{d.blocks, d.part, 0u, 0u};
+  }
   const float scale2 = 1.44269504088896340736f / sqrtf((float)D);   // scores count in powers of two
 
   for (uint32_t u = blockIdx.x; u < total; u += gridDim.x) {
@@ -332,15 +351,6 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     const uint32_t tile = tiles - 1u - w;
     const uint32_t nb = tile_blocks(pos0, T, tile, lg), b0 = chunk * per, b1 = min(nb, b0 + per);
     const uint32_t rows = T << lg, last = pos0 + T - 1u;   // the sequence's last row in the cache
-    // ---- queries: B operand, lane = row, 8 columns a step and half
-    const uint32_t r = tile * kTileRows + wave * 32u + l31, rr = min(r, rows - 1u), t = rr >> lg;
-    const uint32_t head = (kvh << lg) + (rr & ((1u << lg) - 1u)), pos = pos0 + t;
-    u32x4 qf[KS];
-    {
-      const uint16_t* p = a.q + (size_t)(begin + t) * a.q_stride + (size_t)head * D + 8u * half;
-#pragma unroll
-      for (uint32_t k = 0; k < KS; ++k) qf[k] = *as_global((const u32x4*)(p + 16u * k));
-    }
     const uint32_t w0 = tile * kTileRows + wave * 32u;   // the wavefront's rows: none behind `rows`
     const bool have = w0 < rows;
     const uint32_t pos_lo = pos0 + (min(w0, rows - 1u) >> lg), pos_hi = pos0 + (min(w0 + 31u, rows - 1u) >> lg);
@@ -389,6 +399,15 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     fetch_pages(b0);
     request(b0, 0);
     fetch_pages(min(b0 + 1u, b1 - 1u));
+    // ---- queries: B operand, lane = row, 8 columns a step and half
+    const uint32_t r = tile * kTileRows + wave * 32u + l31, rr = min(r, rows - 1u), t = rr >> lg;
+    const uint32_t head = (kvh << lg) + (rr & ((1u << lg) - 1u)), pos = pos0 + t;
+    u32x4 qf[KS];
+    {
+      const uint16_t* p = a.q + (size_t)(begin + t) * a.q_stride + (size_t)head * D + 8u * half;
+#pragma unroll
+      for (uint32_t k = 0; k < KS; ++k) qf[k] = *as_global((const u32x4*)(p + 16u * k));
+    }
 
     f32x16 o[NT];
 #pragma unroll
@@ -531,7 +550,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
           }
       } else {
         const uint32_t held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
-        float* part = (float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)((tile * chunks + chunk) * s.n_kv + kvh) * held * (D + 2u);
+        float* part = (float*)a.work + kAttendHeader + __builtin_amdgcn_readlane(d.part, seq) + (size_t)((tile * chunks + chunk) * s.n_kv + kvh) * held * (D + 2u);
         float* to = part + (size_t)in_tile * D + 4u * half;
 #pragma unroll
         for (uint32_t n = 0; n < NT; ++n)
@@ -549,30 +568,44 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
   __shared__ float weight[4][kAttendMostChunks + 16u];
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
-  const SeqLanes q = load_seqs(s, false);
-  const Deal d = deal_units<D>(s, q, lg);
-  if (!__ballot(d.chunks > 1u)) return;
+  SeqLanes q = {0, 0, -1, 0};
+  uint32_t seq_chunks = 0, blocks = 0, seq_part = 0;
+  if (lane < kMaxRowSeqs) {
+    const u32x4 x = as_global((const u32x4*)a.work)[2u * lane], y = as_global((const u32x4*)a.work)[2u * lane + 1u];
+    q.begin = (int32_t)x[0]; q.end = (int32_t)x[1]; q.pos = (int32_t)x[2];
+    seq_chunks = x[3]; blocks = y[0]; seq_part = y[1];
+  }
+  if (!__ballot(seq_chunks > 1u)) return;
   for (uint64_t item = blockIdx.x * 4u + wave; item < (uint64_t)s.n_rows * s.n_q; item += gridDim.x * 4u) {
   const uint32_t row = (uint32_t)(item / s.n_q), head = (uint32_t)(item - (uint64_t)row * s.n_q);
   const uint32_t seq = seq_of_row(q, row);
   if (seq == 64u) continue;
   const uint32_t T = __builtin_amdgcn_readlane((uint32_t)(q.end - q.begin), seq), pos0 = __builtin_amdgcn_readlane(q.pos, seq);
-  const uint32_t chunks = __builtin_amdgcn_readlane(d.chunks, seq), per = __builtin_amdgcn_readlane(d.blocks, seq);
+  const uint32_t chunks = __builtin_amdgcn_readlane(seq_chunks, seq), per = __builtin_amdgcn_readlane(blocks, seq);
+  if (chunks <= 1u) continue;
   const uint32_t r = ((row - __builtin_amdgcn_readlane(q.begin, seq)) << lg) + (head & ((1u << lg) - 1u)), tile = r / kTileRows;
-  const uint32_t n = (tile_blocks(pos0, T, tile, lg) + per - 1u) / per;
+  const uint32_t n = uniform_u32(quotient(tile_blocks(pos0, T, tile, lg) + per - 1u, per));
   if (n <= 1u) continue;
-  const uint32_t rows = T << lg, held = min(rows, kTileRows), in_tile = r - tile * kTileRows;
-  const uint32_t v0 = tile * chunks * s.n_kv + (head >> lg);
+  const uint32_t held = min(T << lg, kTileRows), in_tile = r - tile * kTileRows;
   const size_t stride = (size_t)s.n_kv * held * (D + 2u);
-  const float* part = (const float*)a.work + __builtin_amdgcn_readlane(d.part, seq) + (size_t)v0 * held * (D + 2u);
-  // the runs' weights, a lane a run (and the 64th, .. after it), into LDS; then the loads of 16 runs are in flight at once
-  float M = -INFINITY, l = 0.f, o[D / 64] = {};
+  const float* part = (const float*)a.work + kAttendHeader + __builtin_amdgcn_readlane(seq_part, seq) +
+                      (size_t)(tile * chunks * s.n_kv + (head >> lg)) * held * (D + 2u);
+  // outputs of 16 runs in flight at once, the first with the maxima and sums, a lane a run (and the 64th, .. after it): their weights go by LDS
+  const float* p = part + (size_t)in_tile * D + (D / 64) * lane;
+  float M = -INFINITY, l = 0.f, o[D / 64] = {}, v[16][D / 64];
   f32x2 ml[kAttendMostChunks / 64];
+  auto request = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t j = 0; j < 16; ++j)
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(c + j, n - 1u) * stride + e];
+  };
 #pragma unroll
   for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
     ml[i] = f32x2{-INFINITY, 0.f};
     if (64u * i + lane < n) ml[i] = *as_global((const f32x2*)(part + (64u * i + lane) * stride + (size_t)held * D + 2u * in_tile));
   }
+  request(0);
 #pragma unroll
   for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) M = fmaxf(M, ml[i].x);
   M = wave_max_dpp(M);
@@ -583,17 +616,14 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
     weight[wave][64u * i + lane] = f;
   }
   l = wave_sum_dpp(l);
-  const float* p = part + (size_t)in_tile * D + (D / 64) * lane;
-  for (uint32_t c = 0; c < n; c += 16u) {
-    float v[16][D / 64];
-#pragma unroll
-    for (uint32_t j = 0; j < 16; ++j)
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(c + j, n - 1u) * stride + e];
+  for (uint32_t c = 0;;) {
 #pragma unroll
     for (uint32_t j = 0; j < 16; ++j)
 #pragma unroll
       for (int e = 0; e < D / 64; ++e) o[e] = c + j < n ? fmaf(v[j][e], weight[wave][c + j], o[e]) : o[e];
+    c += 16u;
+    if (c >= n) break;
+    request(c);
   }
   const float inv = 1.0f / l;
   uint16_t* to = a.out + (size_t)row * a.out_stride + (size_t)head * D + (D / 64) * lane;
