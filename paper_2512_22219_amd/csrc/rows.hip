@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), l31 = lane & 31u, half = lane >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
+  __builtin_amdgcn_s_setprio(3);   // (until the unit's first requests are out: 8 x 1 token 20.3 / 19.6 us)
   const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
   const Deal d = deal_units<D>(s, q, lg);
   const uint32_t total = uniform_u32(d.total);
@@ -423,6 +424,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         const uint32_t place = ((n ^ (D == 128 ? rl : rl >> 1)) << 2) | (un ^ (half + 2u * x));
         vat[n][x] = (8u * x + 4u * half + rl) * ROWB + place * 16u + 8u * (lane & 1u);
       }
+    __builtin_amdgcn_s_setprio(0);
     drain_vmem();
     __syncthreads();
 
@@ -498,11 +500,6 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
           for (uint32_t i = 0; i < 16; ++i) {
             pf[2 * n + (i >> 3)][i & 7u] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[n][i], scale2, -ms));
           }
-#pragma unroll
-        for (uint32_t k = 0; k < 4; ++k)   // the sum is of the rounded ones: the weights add up to one
-#pragma unroll
-          for (uint32_t i = 0; i < 8; i += 2)
-            lsum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[k][i], pf[k][i + 1]}, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
         __builtin_amdgcn_s_setprio(2);
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k)
@@ -516,6 +513,15 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
             o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[k], o[n], 0, 0, 0);
           }
         __builtin_amdgcn_s_setprio(0);
+        // The sum is of the rounded ones: the weights add up to one.  Behind the products, in the shadow of the last of them (in
+        // front of them: 2048 tokens over 14000 992 us instead of 936).
+        float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i += 2)
+#pragma unroll
+          for (uint32_t k = 0; k < 4; ++k)
+            part_sum[k] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[k][i], pf[k][i + 1]}, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, part_sum[k], false);
+        lsum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
         if (__builtin_expect(poisoned, 0)) {
           for (uint32_t j = 0; j < kBlockKeys && kv0 + j <= pos_hi; ++j) {
             size_t at = 0;
@@ -533,6 +539,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
       drain_vmem();
       __syncthreads();
     }
+    __builtin_amdgcn_s_setprio(3);
     // ---- the end: the row's sum of both halves; the output, or the unit's partial result
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
     const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
