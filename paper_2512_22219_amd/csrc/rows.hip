@@ -675,12 +675,11 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------ log probabilities
-// One pass over a row.  A wavefront reads 16 logits a lane and step and keeps, against the largest m that it has seen,
+// One pass over a row.  A wavefront reads N logits a lane and step and keeps, against the largest m that it has seen,
 //   s = sum e^(x - m) without one of the largest, t = sum e^(x - m) (x - m)
 // (ln p = x - m - log1p(s): nothing is lost of a token that is all but certain; entropy = log1p(s) - t / (1 + s)), and its
 // best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
 // With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
-constexpr uint32_t kStep = 1024;          // logits of a wavefront's step
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
 constexpr uint32_t kLogprobWorkgroups = 1024;   // that a call is cut into where its rows are fewer
 constexpr uint32_t kLogprobManyRows = 2048;     // a wavefront a row from here on
@@ -802,7 +801,7 @@ __device__ __forceinline__ float asked_logit(const LogprobArgs& a, uint32_t row)
   return t >= 0 && (uint32_t)t < a.vocab ? logit_at((const T*)a.logits + (size_t)row * a.stride, (size_t)t) : 0.f;
 }
 
-// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [192]) and
+// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [128]) and
 // joined with them 64 at a time: an entry's place is the number of entries above it.  (Put in place one by one, the lanes
 // behind shifted, a row of 151936 with 20 alternatives took 18.8 us instead of 8.7, 4096 rows of 32000 with 4 106 instead of 94.)
 struct Best {
@@ -885,15 +884,15 @@ __device__ __forceinline__ bool join_runs(const LogprobArgs& a, uint32_t row, ui
   return true;
 }
 
-// W wavefronts of a workgroup share a run (4, or 1: a run each).
-template <typename T, uint32_t W>
+// W wavefronts of a workgroup share a run (4, N = 16: a step is what a run has, or 1, N = 16: a whole row each).
+template <typename T, uint32_t W, uint32_t N>
 __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t steps) {
-  constexpr uint32_t E = 16 / sizeof(T), V = 16 / E;   // logits of 16 bytes, such loads of a step
-  __shared__ uint64_t fresh[4][192], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
-  // what hot steps pass from lane to lane (20: reads of 16 logits of four lanes spread over the banks), then the entries of the join
-  __shared__ __align__(16) uint64_t lists[4 * 64 * 20 / 2];
-  float(*offered)[64][20] = (float(*)[64][20])lists;
-  static_assert(sizeof(lists) >= (kLogprobChunks * MPK_ROWS_MAX_TOP + MPK_ROWS_MAX_TOP + 2) * 8, "entries of all runs");
+  constexpr uint32_t E = 16 / sizeof(T), V = N / E, kStep = 64 * N;   // logits of 16 bytes, such loads of a step, logits of a step
+  __shared__ uint64_t fresh[4][128], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
+  // what hot steps pass from lane to lane (4 more: reads of the logits of several lanes spread over the banks), then the entries of the join
+  __shared__ __align__(16) uint64_t lists[4 * 64 * (N + 4) / 2];
+  float(*offered)[64][N + 4] = (float(*)[64][N + 4])lists;
+  static_assert(W == 1 || sizeof(lists) >= (kLogprobChunks * MPK_ROWS_MAX_TOP + MPK_ROWS_MAX_TOP + 2) * 8, "entries of all runs");
   __shared__ RowSum sums[4];
   __shared__ uint32_t bounds[4];
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), part_of = W == 1 ? 0u : wave;
@@ -906,6 +905,10 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   const uint32_t v0 = chunk * steps * (kStep / E), v1 = min(nvec, v0 + steps * (kStep / E));
   float asked = 0.f;
 
+  // The sums count in powers of two from c = log2(e) (m - shift) as rounded, so that an exponent is one fused operation; shift is 0
+  // but for logits so large that the rounding of c would show, which are then taken less it.
+  const float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+  float c = 0.f, shift = 0.f;
   RowSum r = {-INFINITY, 0.f, 0.f};
   Best best;
   float bound = -INFINITY, limit = -INFINITY;   // the row's alternatives are not below the first; the last of the best (nothing to beat without alternatives but the largest)
@@ -920,7 +923,7 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   // The row's edges, what lies in front of the first and behind the last load of 16 bytes, come last, as one step.
   bool edges = false, start = W > 1;
   for (;;) {
-    float y[16];
+    float y[N];
     const uint32_t first = at;
     if (at < v1) {
       u32x4 now[V];
@@ -937,21 +940,22 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
         }
       if (first + kStep / E > v1) {
 #pragma unroll
-        for (uint32_t j = 0; j < 16; ++j)
+        for (uint32_t j = 0; j < N; ++j)
           if (first + (j / E) * 64u + lane >= v1) y[j] = -INFINITY;
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) y[j] = -INFINITY;
+      for (uint32_t j = 0; j < N; ++j) y[j] = -INFINITY;
       if (!start) {
         if (edges || chunk || part_of || !(head + tail)) break;
         edges = true;
       }
       if (edges && lane < head + tail) y[0] = logit_at(x, lane < head ? lane : a.vocab - tail + (lane - head));
     }
-    float mx = y[0];
+    float mx = max3(y[0], y[1], y[2]);
 #pragma unroll
-    for (int j = 1; j < 16; ++j) mx = fmaxf(mx, y[j]);
+    for (uint32_t j = 3; j < N - 1u; j += 2) mx = max3(mx, y[j], y[j + 1]);
+    mx = max3(mx, y[N - 1u], y[N - 1u]);
     float least = -3.402823466e38f;
     const bool equals = edges || start;   // (tokens ascend, so an equal logit does not beat one; the edges come out of order, the bound is a logit)
     if (start) {
@@ -974,13 +978,18 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
       const float m = wave_max_dpp(mx);
       const bool more = m > r.m;
       if (more) {
+        const float sn = fabsf(m) < 1048576.f ? 0.f : m, cn = (m - sn) * kLog2e;
         if (r.m != -INFINITY) {
-          const float d = fmaxf(r.m - m, -200.f), f = __expf(d);
-          if (lane == 0) r.s += 1.f;   // the largest until now is one of many
+          const float d = fmaxf(fmaf(shift - sn, kLog2e, c - cn), -300.f), f = __builtin_amdgcn_exp2f(d);
+          if (lane == 0) {   // the largest until now is one of many
+            const float e = fmaf(r.m - shift, kLog2e, -c), p = __builtin_amdgcn_exp2f(e);
+            r.s += p;
+            r.t = fmaf(p, e, r.t);
+          }
           r.t = fmaf(r.s, d, r.t) * f;
           r.s *= f;
         }
-        r.m = m;
+        r.m = m; c = cn; shift = sn;
       }
       if (k) {
         if ((uint32_t)__popcll(hot) > k) {
@@ -991,27 +1000,21 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
         }
         if (hot >> lane & 1u) {
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) *(float4*)&offered[wave][lane][j] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+          for (uint32_t j = 0; j < N; j += 4) *(float4*)&offered[wave][lane][j] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
         }
-        while (hot) {   // eight such lanes at a time
-          uint32_t from[2] = {64u, 64u};
+        while (hot) {   // four such lanes at a time, or two
+          uint32_t from = 64u;
 #pragma unroll
-          for (uint32_t g = 0; g < 8; ++g) {
-            if (hot && lane >> 4 == (g & 3u)) from[g >> 2] = (uint32_t)__builtin_ctzll(hot);
+          for (uint32_t g = 0; g < 64u / N; ++g) {
+            if (hot && lane / N == g) from = (uint32_t)__builtin_ctzll(hot);
             hot &= hot - 1ull;
           }
-          const uint32_t j = lane & 15u;
-          float v[2];
-#pragma unroll
-          for (uint32_t g = 0; g < 2; ++g) v[g] = offered[wave][from[g] & 63u][j];
-#pragma unroll
-          for (uint32_t g = 0; g < 2; ++g) {
-            const uint32_t l = from[g], token = edges ? (l < head ? l : a.vocab - tail + (l - head)) : head + (first + (j / E) * 64u + l) * E + j % E;
-            const uint64_t e = entry_of(v[g], token), b = __ballot(l < 64u && v[g] >= least && e > best.last);
-            if (!b) continue;
-            if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
-            best.waiting += (uint32_t)__popcll(b);
-          }
+          const uint32_t j = lane % N;
+          const float v = offered[wave][from & 63u][j];
+          const uint32_t token = edges ? (from < head ? from : a.vocab - tail + (from - head)) : head + (first + (j / E) * 64u + from) * E + j % E;
+          const uint64_t e = entry_of(v, token), b = __ballot(from < 64u && v >= least && e > best.last);
+          if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
+          best.waiting += (uint32_t)__popcll(b);
           if (best.waiting >= 64u || !hot) best.join(fresh[wave], sorted[wave], k);
         }
         limit = fmaxf(bound, best.last ? entry_logit(best.last) : -INFINITY);
@@ -1019,20 +1022,23 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
       if (more) {   // one of the largest stays out of the sum
         bool out = lane == (uint32_t)__builtin_ctzll(__ballot(mx == m));
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (uint32_t j = 0; j < N; ++j) {
           const bool it = out && y[j] == m;
           y[j] = it ? -INFINITY : y[j];
           out = out && !it;
         }
       }
     }
-    const float m = r.m == -INFINITY ? 0.f : r.m;
+    if (__builtin_expect(shift != 0.f, 0)) {
+#pragma unroll
+      for (uint32_t j = 0; j < N; ++j) y[j] -= shift;
+    }
     float s = 0.f, t = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float d = y[j] - m, e = __expf(d);
+    for (uint32_t j = 0; j < N; ++j) {
+      const float d = fmaf(y[j], kLog2e, -c), e = __builtin_amdgcn_exp2f(d);
       s += e;
-      t = fmaf(e, fmaxf(d, -200.f), t);
+      t = fmaf(e, fmaxf(d, -300.f), t);
     }
     r.s += s;
     r.t += t;
@@ -1040,6 +1046,11 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   // ---- the lanes' and the wavefronts' results together
   r.s = wave_sum_dpp(r.s);
   r.t = wave_sum_dpp(r.t);
+  if (r.m != -INFINITY) {   // from powers of two and c to those of e and m
+    const float e = fmaf(r.m - shift, kLog2e, -c), f = __builtin_amdgcn_exp2f(-e);
+    r.t = fmaf(-e, r.s, r.t) * f * kLn2;
+    r.s *= f;
+  }
   uint64_t mine = best.mine;
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = r;
@@ -1062,12 +1073,13 @@ template <typename T>
 static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   // a workgroup's share: a whole row where there are rows enough for all compute units, 4096 logits or more
   if (a.n_rows >= kLogprobManyRows) {
-    rows_logprobs_kernel<T, 1><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, (a.vocab + kStep - 1u) / kStep + 1u);
+    rows_logprobs_kernel<T, 1, 16><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, a.vocab / (64u * 16) + 1u);
     return hipGetLastError();
   }
-  const uint32_t all = std::max(1u, (a.vocab + 4u * kStep - 1u) / (4u * kStep)), want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
+  constexpr uint32_t kRound = 4u * 64u * 16u;   // logits that a workgroup takes at once
+  const uint32_t all = (a.vocab + kRound - 1u) / kRound, want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
   const uint32_t n = std::min(std::min(want, all), kLogprobChunks), steps = 4u * ((all + n - 1u) / n), chunks = (4u * all + steps - 1u) / steps;
-  rows_logprobs_kernel<T, 4><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, steps);
+  rows_logprobs_kernel<T, 4, 16><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, steps);
   return hipGetLastError();
 }
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream) {
