@@ -195,8 +195,9 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 // K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
-constexpr uint32_t kAttendMinBlocks = 2, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
-constexpr uint32_t kAttendWhole = 6;   // blocks that are not cut
+constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
+constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
+constexpr float kAttendShare = 1.8e-4f;      // ... and a row's partial result
 constexpr uint32_t kJoinWorkgroups = 1024;
 constexpr uint32_t kAttendHeader = 1024;   // floats of the workspace in front of the partial results
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
@@ -256,10 +257,16 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
   // few tiles: at most as many units as run at once, all about as long
   uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots)));
+  // A run more is a partial result more of every tile, written and read: in blocks' time `share`, with all tiles of the call; and the
+  // first cut is a second kernel.  So a run is no shorter than the square root that has blocks and partial results cost the same,
+  // and a tile is cut only where that saves more than it costs.  (Cut into as many runs as run at once / as here: 512 tokens 25.6 /
+  // 17.6 us, eight times 200 over 300 51 / 24; tiles of up to 22 blocks never cut / as here: 64 tokens over 1000 27.6 / 15.3.)
   const uint32_t held = min(rows, kTileRows);
-  c = max(c, kAttendMinBlocks);
+  const float share = (float)(few * held) * kAttendShare;
+  c = max(max(c, kAttendMinBlocks), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
-    d.chunks = nb > max(c, kAttendWhole) ? quotient(nb + c - 1u, c) : 1u;
+    d.chunks = quotient(nb + c - 1u, c);
+    if ((float)nb < (float)c + (float)kAttendJoinBlocks + share * (float)d.chunks) d.chunks = 1u;
     const bool cut = T && d.chunks > 1u;
     const float need = cut ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(held * (D + 2u)) : 0.f;
     if (uniform_f32(row16_reduce(need, add)) <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u) && __all(d.chunks <= kAttendMostChunks)) break;
@@ -660,10 +667,10 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   // units: one per tile, and up to kAttendSlots more where tiles are cut (a workgroup without one has worked that out for nothing;
   // one takes several where there are more)
   const uint64_t tiles = (((uint64_t)a.s.n_rows << lg) / kTileRows + a.s.n_seqs) * a.s.n_kv;
-  const uint32_t grid = tiles <= kAttendSlots / 2u ? kAttendSlots : (uint32_t)std::min<uint64_t>(tiles + kAttendSlots / 4u, 1u << 20);
+  const uint32_t grid = (uint32_t)std::min<uint64_t>(tiles <= kAttendSlots / 2u ? kAttendSlots : tiles + (tiles <= 2u * kAttendSlots ? kAttendSlots : kAttendSlots / 4u), 1u << 20);
   rows_attend_kernel<D, PAGED><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.s.max_seq <= kAttendWhole * kBlockKeys) return e;
+  if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
   rows_attend_join_kernel<D><<<dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
   return hipGetLastError();
 }
