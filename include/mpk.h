@@ -556,6 +556,10 @@ void mpk_serve_destroy(mpk_server *s);
  *     out of range) is reported by mpk_graph_status as MPK_ERR_DEVICE, never dereferenced; the
  *     sequence or row concerned is left out (details below).  The error word keeps the first error
  *     until mpk_graph_reset.
+ *   - errors: INVALID_ARG (a NULL or misaligned pointer, a stride too short or no multiple of 8, an
+ *     unknown type, a count out of range, a graph that cannot run them), UNSUPPORTED (max_seq above
+ *     2^28), HIP.  n_rows is at most 2^24; a call of no rows does nothing and takes NULL for what
+ *     would have n_rows rows.
  *   - results do not depend on timing: the same call gives the same bits.
  * -------------------------------------------------------------------------------------------- */
 typedef enum { MPK_ROWS_BF16 = 0, MPK_ROWS_F32 = 1 } mpk_rows_type;
@@ -568,7 +572,7 @@ typedef enum { MPK_ROWS_BF16 = 0, MPK_ROWS_F32 = 1 } mpk_rows_type;
 /* Query/key norm (MPK_MODEL_QK_NORM), position rotation, append to the KV cache.
  *   layer     : the layer whose cache rows are written and whose q_norm / k_norm are used
  *   n_seqs    : sequences of this call, 1 .. batch
- *   n_rows    : rows that qkv and q_out have (0: nothing to do)
+ *   n_rows    : rows that qkv and q_out have
  *   row_begin : device int32 [n_seqs + 1], ascending, within 0 .. n_rows: sequence i has rows
  *               row_begin[i] .. row_begin[i + 1] - 1 (possibly none).  Rows before the first and
  *               behind the last sequence are neither read nor written
@@ -581,7 +585,7 @@ typedef enum { MPK_ROWS_BF16 = 0, MPK_ROWS_F32 = 1 } mpk_rows_type;
  *               aligned, strides multiples of 8 elements
  *   q_out     : device bf16 [n_rows][row stride q_stride elements], n_q_heads head_dim a row: the
  *               queries, normed and rotated.  May be qkv itself with the same stride (bf16): the
- *               queries are then rotated in place
+ *               queries are then rotated in place; no other overlap
  * K and V rows are written to the cache as a decode step writes them: fp32 arithmetic, angles in fp64,
  * rounded to bf16 once.  A paged cache's rows go to the pages the table names for them.
  * Device errors: row_begin not ascending or outside 0 .. n_rows (nothing is written); a slot outside
@@ -597,8 +601,8 @@ mpk_status mpk_rows_append(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  *   layer .. positions : as above
  *   q   : device bf16 [n_rows][row stride q_stride], n_q_heads head_dim a row, as mpk_rows_append leaves
  *         them (q_out, or qkv rotated in place)
- *   out : device bf16 [n_rows][row stride out_stride], n_q_heads head_dim a row; not q.  16-byte aligned,
- *         strides multiples of 8 elements
+ *   out : device bf16 [n_rows][row stride out_stride], n_q_heads head_dim a row; no overlap with q.
+ *         16-byte aligned, strides multiples of 8 elements
  *   workspace : device, MPK_ROWS_WORKSPACE_BYTES
  * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the product with
  * V, the output once at the end.  Cache rows above a row's position never reach it, whatever they hold
@@ -612,7 +616,7 @@ mpk_status mpk_rows_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
 /* What rows of logits say: with p = softmax(row) over the graph's vocab,
  *   logits       : device [n_rows][row stride row_stride elements], bf16 or fp32 (logits_type): what a
  *                  decode step writes, logits_all of mpk_decode_steps, an LM head over prompt rows.  Any
- *                  alignment of the element type, any stride >= vocab; n_rows 0: nothing to do
+ *                  alignment of the element type, any stride >= vocab
  *   tokens       : device int32 [n_rows]: the token asked about, -1: none (its logprob is 0)
  *   logprobs     : device fp32 [n_rows]: ln p[token]   (tokens and logprobs: both or neither NULL)
  *   entropy      : device fp32 [n_rows] or NULL: -sum p ln p, in nats

@@ -55,8 +55,8 @@ struct LogprobArgs {
   uint32_t *err, *arrivals;
 };
 
-// Once per device, before any of the others: what the kernels need beyond the defaults.
-hipError_t rows_prepare();
+// Before any of the others, with the device current: what the kernels need beyond the defaults, once per device.
+hipError_t rows_prepare(int device);
 // Each checks nothing (the entry points have) and launches on `stream`.
 hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream);

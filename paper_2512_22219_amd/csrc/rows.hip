@@ -235,7 +235,7 @@ __device__ __forceinline__ uint32_t row16_before(uint32_t v) {
   add(std::integral_constant<int, 0x118>{});
   return x - v;
 }
-// n / d for n below 2^24 (blocks of keys: max_seq is below 2^30).  The compiler's division, right for any number, is forty
+// n / d for n below 2^24 (blocks of keys: the host refuses a max_seq above 2^28).  The compiler's division, right for any number, is forty
 // operations, and there were six in front of a call's first load.
 __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d) {
   uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
@@ -262,7 +262,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   // and a tile is cut only where that saves more than it costs.  (Cut into as many runs as run at once / as here: 512 tokens 25.6 /
   // 17.6 us, eight times 200 over 300 51 / 24; tiles of up to 22 blocks never cut / as here: 64 tokens over 1000 27.6 / 15.3.)
   const uint32_t held = min(rows, kTileRows);
-  const float share = (float)(few * held) * kAttendShare;
+  const float share = (float)few * (float)held * kAttendShare;
   c = max(max(c, kAttendMinBlocks), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
     d.chunks = quotient(nb + c - 1u, c);
@@ -655,10 +655,18 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
 }
 
 constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
-hipError_t rows_prepare() {
+hipError_t rows_prepare(int device) {
+  static std::mutex mu;
+  static std::vector<bool> done;
+  std::lock_guard<std::mutex> lock(mu);
+  if ((size_t)device < done.size() && done[device]) return hipSuccess;
   hipError_t e = hipSuccess;
   for (const void* fn : {(const void*)rows_attend_kernel<128, false>, (const void*)rows_attend_kernel<128, true>})
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_lds(128));
+  if (e == hipSuccess) {
+    done.resize(std::max(done.size(), (size_t)device + 1u));
+    done[device] = true;
+  }
   return e;
 }
 

@@ -518,7 +518,7 @@ extern "C" mpk_status mpk_compile(const mpk_model_config* cfg, const mpk_weight_
       if ((st = upload(&g->d_const_static, csv)) != MPK_OK) return fail(st);
     }
   }
-  if ((e = rows_prepare()) != hipSuccess) { set_error("cannot reserve LDS for the calls on rows: %s", hipGetErrorString(e)); return fail(MPK_ERR_HIP); }
+  if ((e = rows_prepare(g->device)) != hipSuccess) { set_error("cannot reserve LDS for the calls on rows: %s", hipGetErrorString(e)); return fail(MPK_ERR_HIP); }
   g->cache_k = (uint16_t*)kv->k;
   g->cache_v = (uint16_t*)kv->v;
   const bool qk_norm = (cfg->flags & MPK_MODEL_QK_NORM) != 0;
@@ -1116,6 +1116,7 @@ extern "C" void mpk_serve_destroy(mpk_server* s) {
 
 // ------------------------------------------------------------------ rows beside the decode step
 // Arguments are looked at first, whether the graph can run anything last: what a call refuses can be tried without a GPU.
+// Buffers of no rows are not looked at: an empty tensor has no address.
 static mpk_status rows_runnable(const mpk_graph* g) {
   if (g->h.opt.serving) { set_error("a serving graph's slots and pages belong to its server"); return MPK_ERR_INVALID_ARG; }
   if (g->host_only) { set_error("graph was compiled host_only"); return MPK_ERR_INVALID_ARG; }
@@ -1134,6 +1135,7 @@ static mpk_status rows_work(const void* workspace) {
   return MPK_OK;
 }
 constexpr uint32_t kRowsMost = 1u << 24;   // rows of a call
+constexpr uint32_t kRowsMostSeq = 1u << 28;   // max_seq of the graph
 static mpk_status rows_count(uint32_t n_rows) {
   if (n_rows > kRowsMost) { set_error("n_rows %u is above %u", n_rows, kRowsMost); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
@@ -1145,6 +1147,7 @@ static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs,
   if (h.cfg.batch == 0) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
   if (layer >= h.cfg.n_layers) { set_error("layer %u, the model has %u", layer, h.cfg.n_layers); return MPK_ERR_INVALID_ARG; }
   if (n_seqs == 0 || n_seqs > std::min(h.cfg.batch, kMaxRowSeqs)) { set_error("n_seqs %u is outside 1..%u, the graph's batch", n_seqs, h.cfg.batch); return MPK_ERR_INVALID_ARG; }
+  if (h.cfg.max_seq > kRowsMostSeq) { set_error("max_seq %u is above %u", h.cfg.max_seq, kRowsMostSeq); return MPK_ERR_UNSUPPORTED; }
   const mpk_status st = rows_count(n_rows);
   if (st != MPK_OK) return st;
   *s = RowSeqs{};
@@ -1180,10 +1183,11 @@ extern "C" mpk_status mpk_rows_append(mpk_graph* g, uint32_t layer, uint32_t n_s
   if (st != MPK_OK) return st;
   if (qkv_type > MPK_ROWS_F32) { set_error("unknown qkv_type %u", qkv_type); return MPK_ERR_INVALID_ARG; }
   const size_t q = (size_t)a.s.n_q * a.s.head_dim;
+  if (!n_rows) return rows_cache_runnable(g);
   if ((st = rows_buffer("qkv", qkv, qkv_stride, q + 2 * (size_t)a.s.n_kv * a.s.head_dim)) != MPK_OK) return st;
   if ((st = rows_buffer("q_out", q_out, q_stride, q)) != MPK_OK) return st;
   if (qkv == q_out && (qkv_type != MPK_ROWS_BF16 || qkv_stride != q_stride)) { set_error("queries are rotated in place in bf16 rows of one stride only"); return MPK_ERR_INVALID_ARG; }
-  if ((st = rows_cache_runnable(g)) != MPK_OK || !n_rows) return st;
+  if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
   a.qkv = qkv; a.qkv_stride = qkv_stride;
   a.q_out = (uint16_t*)q_out; a.q_stride = q_stride;
   a.q_norm = g->qk_gains[layer].first; a.k_norm = g->qk_gains[layer].second;
@@ -1198,12 +1202,13 @@ extern "C" mpk_status mpk_rows_attend(mpk_graph* g, uint32_t layer, uint32_t n_s
   AttendArgs a{};
   mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
   if (st != MPK_OK) return st;
+  if (!n_rows) return rows_cache_runnable(g);
   const size_t width = (size_t)a.s.n_q * a.s.head_dim;
   if ((st = rows_buffer("q", q, q_stride, width)) != MPK_OK) return st;
   if ((st = rows_buffer("out", out, out_stride, width)) != MPK_OK) return st;
   if (q == out) { set_error("out is q"); return MPK_ERR_INVALID_ARG; }
   if ((st = rows_work(workspace)) != MPK_OK) return st;
-  if ((st = rows_cache_runnable(g)) != MPK_OK || !n_rows) return st;
+  if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
   a.q = (const uint16_t*)q; a.q_stride = q_stride;
   a.out = (uint16_t*)out; a.out_stride = out_stride;
   a.work = workspace;
@@ -1218,14 +1223,16 @@ extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const voi
   const uint32_t vocab = g->h.cfg.vocab;
   if (!vocab) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
   if (logits_type > MPK_ROWS_F32) { set_error("unknown logits_type %u", logits_type); return MPK_ERR_INVALID_ARG; }
+  if (n_top > std::min(MPK_ROWS_MAX_TOP, vocab)) { set_error("n_top %u is above %u", n_top, std::min(MPK_ROWS_MAX_TOP, vocab)); return MPK_ERR_INVALID_ARG; }
+  mpk_status st = rows_count(n_rows);
+  if (st != MPK_OK) return st;
+  if (!n_rows) return rows_runnable(g);
   if (!logits || (uintptr_t)logits % (logits_type == MPK_ROWS_F32 ? 4 : 2)) { set_error("logits is NULL or not aligned to its elements"); return MPK_ERR_INVALID_ARG; }
   if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
   if (!tokens != !logprobs) { set_error("tokens and logprobs: both or neither"); return MPK_ERR_INVALID_ARG; }
-  if (n_top > std::min(MPK_ROWS_MAX_TOP, vocab)) { set_error("n_top %u is above %u", n_top, std::min(MPK_ROWS_MAX_TOP, vocab)); return MPK_ERR_INVALID_ARG; }
   if (n_top && (!top_tokens || !top_logprobs)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
-  mpk_status st = rows_count(n_rows);
-  if (st != MPK_OK || (st = rows_work(workspace)) != MPK_OK) return st;
-  if ((st = rows_runnable(g)) != MPK_OK || !n_rows || (!tokens && !entropy && !n_top)) return st;
+  if ((st = rows_work(workspace)) != MPK_OK) return st;
+  if ((st = rows_runnable(g)) != MPK_OK || (!tokens && !entropy && !n_top)) return st;
   LogprobArgs a{};
   a.logits = logits; a.stride = row_stride;
   a.tokens = tokens; a.logprobs = logprobs; a.entropy = entropy;

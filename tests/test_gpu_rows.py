@@ -1,4 +1,6 @@
 """mpk_rows_append and mpk_rows_attend on the GPU against 64-bit results."""
+import random
+
 import pytest
 import torch
 
@@ -142,6 +144,51 @@ def test_attend(case, pad):
     m.attend(layer, begin, slots, pos, q, out, workspace())
     m.status()
     _check_attend(m, layer, lens, pos, slots, begin, q, out, before)
+
+
+def _random_case(seed):
+    rng = random.Random(seed)
+    n_kv, n = rng.choice([1, 2, 3, 8]), rng.choice([1, 2, 3, 7, 16])
+    c = dict(n_kv=n_kv, n_q=n_kv * rng.choice([1, 2, 4, 8]), d=rng.choice([64, 128]), batch=n, layers=1, page=rng.choice([0, 8, 16, 32, 64, 256]),
+             first=rng.choice([0, 3]), behind=rng.choice([0, 5]))
+    most = rng.choice([1, 4, 40, 300]) if n > 3 else rng.choice([1, 9, 130, 900])
+    c["lens"] = [rng.choice([0, 1, rng.randint(0, most)]) for _ in range(n)]
+    c["pos"] = [rng.choice([0, rng.randint(0, 200), rng.randint(0, 4000)]) for _ in range(n)]
+    step = c["page"] or 1
+    c["max_seq"] = -(-max(a + b for a, b in zip(c["lens"], c["pos"])) // step) * step or step
+    if c["page"]:
+        c["pages"] = n * c["max_seq"] // c["page"] + 3
+    c["slots"] = rng.sample(range(n), n)
+    return c
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_appends_and_attention(seed):
+    case = _random_case(seed)
+    m, lens, pos, slots, begin, _ = _attend_case(case, seed=seed)
+    rows, width = begin[-1] + case["behind"], m.n_q * m.d
+    x = m.normal(rows, (m.n_q + 2 * m.n_kv) * m.d)
+    q, out, k0, v0 = m.normal(rows, width), m.normal(rows, width), m.k.clone(), m.v.clone()
+    before, q_before = out.clone(), q.clone()
+    m.append(0, begin, slots, pos, x, q)
+    m.attend(0, begin, slots, pos, q, out, workspace())
+    m.status()
+    _check_attend(m, 0, lens, pos, slots, begin, q, out, before)
+    written = 0
+    for i, (n, p) in enumerate(zip(lens, pos)):
+        r = slice(begin[i], begin[i + 1])
+        q_before[r] = q[r]
+        if n:
+            at = torch.arange(p, p + n, device=m.dev)
+            want, wk, _, size, ksize = append_exact(m, 0, at, x[r])
+            noise = (m.d / 4 + 16) * F32_HALF
+            assert ((q[r].view(n, m.n_q, m.d).double() - want).abs() <= BF16_HALF * want.abs() + noise * size).all()
+            got = m.cached(m.k, 0, slots[i], p + n)[:, p:].transpose(0, 1).double()
+            assert ((got - wk).abs() <= BF16_HALF * wk.abs() + noise * ksize).all()
+            assert torch.equal(_bits(m.cached(m.v, 0, slots[i], p + n)[:, p:].transpose(0, 1)), _bits(x[r].view(n, -1, m.d)[:, m.n_q + m.n_kv:]))
+            written += n * m.n_kv * m.d
+    assert torch.equal(_bits(q_before), _bits(q))
+    assert (_bits(m.k) != _bits(k0)).sum() <= written and (_bits(m.v) != _bits(v0)).sum() <= written
 
 
 @pytest.mark.parametrize("scale", [0.0, 30.0])

@@ -101,6 +101,18 @@ def test_ties_and_orders(kind, rows, vocab):
     _check(vocab, x, tokens, 20)
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 30011), (3, 8000), (2100, 1000)])
+@pytest.mark.parametrize("level", [1e4, 1.0e6, 1.1e6, 3e7, 1e12, 1e30])
+def test_large_logits(level, rows, vocab):
+    """Around `level`, in steps of its last place: a row may rise from small logits to these."""
+    x, tokens = _inputs(rows, vocab, torch.float32, 8)
+    step = torch.finfo(torch.float32).eps * level
+    x = (level + (x * max(1.0, 2 * step)).round())
+    x[0, : vocab // 3] = torch.arange(vocab // 3, device="cuda") * 1e-3
+    x[rows - 1] = -x[rows - 1]
+    _check(vocab, x, tokens, 20)
+
+
 @pytest.mark.parametrize("vocab", [1000, 30011, 151936])
 def test_ruled_out_tokens(vocab):
     x, tokens = _inputs(6, vocab, torch.float32, 1)

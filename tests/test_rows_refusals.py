@@ -59,6 +59,25 @@ def test_fewer_tokens_than_alternatives():
     _refused(g.rows_logprobs, *dict(LOGITS, n_top=8).values(), match="host_only")
 
 
+def test_no_rows_need_no_buffers():
+    """An empty tensor has no address; what else the call says is still looked at."""
+    g = RowsModel(host_only=True).graph
+    append, attend, logits = dict(APPEND, n_rows=0, qkv=0, q_out=0), dict(ATTEND, n_rows=0, q=0, out=0), dict(LOGITS, n_rows=0, logits=0)
+    for call, args in ((g.rows_append, append), (g.rows_attend, attend), (g.rows_logprobs, logits)):
+        _refused(call, *args.values(), match="host_only")
+    _refused(g.rows_append, *dict(append, n_seqs=0).values(), match="n_seqs")
+    _refused(g.rows_attend, *dict(attend, layer=9).values(), match="layer")
+
+
+def test_a_cache_too_long_for_the_cuts():
+    g = RowsModel(max_seq=(1 << 28) + 8, batch=1, host_only=True).graph
+    for call in (lambda: g.rows_append(*APPEND.values()), lambda: g.rows_attend(*ATTEND.values())):
+        with pytest.raises(M.MpkError, match="max_seq") as e:
+            call()
+        assert e.value.status == M.MPK_ERR_UNSUPPORTED
+    _refused(g.rows_logprobs, *LOGITS.values(), match="host_only")
+
+
 def test_a_serving_graph_and_a_task_dag():
     g = RowsModel(page=16, pages=99, serving=1, greedy_loop=1, host_only=True).graph
     _refused(g.rows_append, *APPEND.values(), match="server")
