@@ -255,7 +255,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   const uint32_t nb = T ? ((uint32_t)q.pos + T + kBlockKeys - 1u) / kBlockKeys : 0u;
   const uint32_t few = row16_reduce(d.tiles, add) * s.n_kv;
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
-  // few tiles: at most as many units as run at once, all about as long
+  // few tiles: at most as many units as run at once, all about as long (in 32 bits; no sequence has 2^22 blocks)
   uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots)));
   // A run more is a partial result more of every tile, written and read: in blocks' time `share`, with all tiles of the call; and the
   // first cut is a second kernel.  So a run is no shorter than the square root that has blocks and partial results cost the same,
@@ -263,7 +263,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   // 17.6 us, eight times 200 over 300 51 / 24; tiles of up to 22 blocks never cut / as here: 64 tokens over 1000 27.6 / 15.3.)
   const uint32_t held = min(rows, kTileRows);
   const float share = (float)few * (float)held * kAttendShare;
-  c = max(max(c, kAttendMinBlocks), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
+  c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
     d.chunks = quotient(nb + c - 1u, c);
     if ((float)nb < (float)c + (float)kAttendJoinBlocks + share * (float)d.chunks) d.chunks = 1u;

@@ -1,5 +1,6 @@
 """mpk_rows_append and mpk_rows_attend on the GPU against 64-bit results."""
 import random
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -248,6 +249,78 @@ def test_an_infinite_or_nan_value_reaches_the_rows_that_see_it():
     want[80:, :4, 3] = True
     want[100:, 4:, 70] = True
     assert torch.equal(~torch.isfinite(o), want) and (o[80:, :4, 3] == float("inf")).all() and o[100:, 4:, 70].isnan().all()
+
+
+@pytest.mark.parametrize("page", [0, 4096])
+def test_a_cache_whose_offsets_pass_32_bits(page):
+    """2^25 positions of 128 elements (smaller pages would be more of them than a decode step can hold).  All keys are zero but
+    three, at the start, in the middle and at the end; their scores, 40, leave the others together less than 3.4e7 e^-40,
+    2e-10, of the weight."""
+    n, pos = (1 << 25) + 4096, (1 << 25) + 900
+    pages = dict(page=page, pages=n // page) if page else {}
+    m = RowsModel(n_q=2, n_kv=1, d=128, layers=1, batch=1, max_seq=n, fill=0.0, **pages)
+    x = m.normal(3, 4 * 128)
+    rotated, out = m.normal(3, 256), m.normal(3, 256)
+    m.append(0, [0, 3], None, [pos], x, rotated)
+    m.status()
+    want, wk, _, size, ksize = append_exact(m, 0, torch.arange(pos, pos + 3, device=m.dev), x)
+    noise = (128 / 4 + 16) * F32_HALF
+
+    def row(cache, at):
+        return cache[0, 0, 0, at] if not page else cache[0, int(m.table[0, at // page]), 0, at % page]
+
+    assert ((rotated.view(3, 2, 128).double() - want).abs() <= BF16_HALF * want.abs() + noise * size).all()
+    assert sum(int(torch.count_nonzero(c)) for c in m.v[0].split(1 << 14, 0)) <= 3 * 128
+    for i in range(3):
+        assert ((row(m.k, pos + i).double() - wk[i, 0]).abs() <= BF16_HALF * wk[i, 0].abs() + noise * ksize[i, 0]).all()
+        assert torch.equal(_bits(row(m.v, pos + i)), _bits(x[i, 3 * 128:]))
+        row(m.k, pos + i).zero_()
+    queries = torch.zeros(3, 256, dtype=torch.bfloat16, device=m.dev)
+    queries[:, 0] = queries[:, 128] = 64.0
+    seen = [5, (1 << 24) + 77, pos + 1]
+    for at in seen:
+        row(m.k, at)[0] = 40 * 128 ** 0.5 / 64
+        row(m.v, at).copy_(m.normal(128))
+    m.attend(0, [0, 3], None, [pos], queries, out, workspace())
+    m.status()
+    for i in range(3):
+        v = torch.stack([row(m.v, at) for at in seen if at <= pos + i]).double()
+        # weights as they are rounded to bf16 against their sum, and the output once
+        bound = 2 * BF16_HALF * v.abs().mean(0) + BF16_HALF * v.mean(0).abs() + 1e-6
+        assert ((out[i].view(2, 128).double() - v.mean(0)).abs() <= bound).all()
+
+
+def test_two_graphs_at_once():
+    """Each on a stream of its own, with a workspace of its own."""
+    case = dict(n_q=8, n_kv=2, d=128, batch=3, layers=1, max_seq=4096, page=0, lens=[1, 70, 3], pos=[4000, 1300, 9], slots=[0, 1, 2],
+                first=0, behind=0)
+    sides = []
+    for seed in (1, 2):
+        m, lens, pos, slots, begin, _ = _attend_case(case, seed=seed)
+        q, logits = m.normal(begin[-1], m.n_q * m.d), m.normal(5, m.vocab, dtype=torch.float32)
+        sides.append(SimpleNamespace(m=m, q=q, logits=logits, tokens=m.ints([3] * 5), work=workspace(), stream=torch.cuda.Stream(),
+                                     lists=(m.ints(begin), m.ints(pos)), outs=[]))
+
+    def run(s, stream):
+        with torch.cuda.stream(stream):
+            out, lp, ent = torch.empty_like(s.q), torch.empty(5, device="cuda"), torch.empty(5, device="cuda")
+            s.m.graph.rows_attend(0, 3, len(s.q), s.lists[0].data_ptr(), 0, s.lists[1].data_ptr(), s.q.data_ptr(), s.q.stride(0),
+                                  out.data_ptr(), out.stride(0), s.work.data_ptr(), stream.cuda_stream)
+            s.m.graph.rows_logprobs(5, s.logits.data_ptr(), M.ROWS_F32, s.m.vocab, s.tokens.data_ptr(), 0, lp.data_ptr(), ent.data_ptr(),
+                                    0, 0, s.work.data_ptr(), stream.cuda_stream)
+        return out, lp, ent
+
+    alone = []
+    for s in sides:
+        alone.append(run(s, torch.cuda.current_stream()))
+        s.m.status()
+    for _ in range(20):
+        for s in sides:
+            s.outs.append(run(s, s.stream))
+    for s, want in zip(sides, alone):
+        s.m.status()
+        for got in s.outs:
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_the_same_call_gives_the_same_bits_on_any_stream():
