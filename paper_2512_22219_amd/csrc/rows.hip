@@ -816,12 +816,21 @@ __device__ __forceinline__ float asked_logit(const LogprobArgs& a, uint32_t row)
   return t >= 0 && (uint32_t)t < a.vocab ? logit_at((const T*)a.logits + (size_t)row * a.stride, (size_t)t) : 0.f;
 }
 
-// A wavefront's best entries so far: lane j holds the j-th.  What a step has to offer is gathered in LDS (fresh [128]) and
-// joined with them 64 at a time: an entry's place is the number of entries above it.  (Put in place one by one, the lanes
-// behind shifted, a row of 151936 with 20 alternatives took 18.8 us instead of 8.7, 4096 rows of 32000 with 4 106 instead of 94.)
+// A wavefront's best entries so far: lane j holds the j-th.  A few that a step has to offer are put in place one by one, the
+// lanes behind shifted.  More are gathered in LDS (fresh [128]) and joined with them 64 at a time: an entry's place is the
+// number of entries above it.  (All joined / up to kLogprobFew put in place, 4096 rows of 32000: 4 alternatives 63.7 / 59.5 us, 20
+// 89 / 75; 2048 rows of 151936 with 20 180 / 150.  With up to 1, 4, 16 or 64: 84, 77, 76, 75 and 159, 149, 150, 150.)
+constexpr uint32_t kLogprobFew = 8;
 struct Best {
   uint64_t mine = 0, last = 0;   // last: the n_top-th, 0 while there are fewer
   uint32_t count = 0, waiting = 0;
+  __device__ __forceinline__ void insert(uint64_t e, uint32_t n_top) {
+    const uint32_t lane = threadIdx.x & 63u, place = (uint32_t)__popcll(__ballot(mine > e));
+    auto lane_before = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x138, 0xF, 0xF, true); };   // wave_shr 1
+    const uint64_t before = (uint64_t)lane_before((uint32_t)(mine >> 32)) << 32 | lane_before((uint32_t)mine);
+    count = min(n_top, count + 1u);
+    mine = lane >= count ? 0 : lane == place ? e : lane > place ? before : mine;
+  }
   __device__ __forceinline__ void join(uint64_t* fresh, uint64_t* sorted, uint32_t n_top) {
     const uint32_t lane = threadIdx.x & 63u;
     for (uint32_t at = 0; at < waiting; at += 64u) {
@@ -1027,7 +1036,14 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
           const uint32_t j = lane % N;
           const float v = offered[wave][from & 63u][j];
           const uint32_t token = edges ? (from < head ? from : a.vocab - tail + (from - head)) : head + (first + (j / E) * 64u + from) * E + j % E;
-          const uint64_t e = entry_of(v, token), b = __ballot(from < 64u && v >= least && e > best.last);
+          const uint64_t e = entry_of(v, token);
+          uint64_t b = __ballot(from < 64u && v >= least && e > best.last);
+          if (!best.waiting && !hot && (uint32_t)__popcll(b) <= kLogprobFew) {
+            for (; b; b &= b - 1ull) best.insert(readlane64(e, (uint32_t)__builtin_ctzll(b)), k);
+            if (lane < best.count) sorted[wave][lane] = best.mine;
+            best.last = best.count == k ? readlane64(best.mine, k - 1u) : 0;
+            break;
+          }
           if (b >> lane & 1u) fresh[wave][best.waiting + (uint32_t)__popcll(b & ((1ull << lane) - 1u))] = e;
           best.waiting += (uint32_t)__popcll(b);
           if (best.waiting >= 64u || !hot) best.join(fresh[wave], sorted[wave], k);
