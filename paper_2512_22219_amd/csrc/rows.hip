@@ -742,7 +742,7 @@ __device__ __forceinline__ void rank_entries(const uint64_t* list, uint32_t n, u
     const uint32_t i = i0 + (threadIdx.x >> 3);
     const uint64_t mine = i < n ? list[i] : 0;
     uint32_t rank = 0;
-#pragma unroll 2
+#pragma unroll 4
     for (uint32_t j = threadIdx.x & 7u; j < n; j += 8u) rank += list[j] > mine;
     rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0xB1, 0xF, 0xF, true);    // lane ^ 1
     rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0x4E, 0xF, 0xF, true);    // lane ^ 2
@@ -910,7 +910,7 @@ __device__ __forceinline__ bool join_runs(const LogprobArgs& a, uint32_t row, ui
 
 // W wavefronts of a workgroup share a run (4, N = 16: a step is what a run has, or 1, N = 16: a whole row each).
 template <typename T, uint32_t W, uint32_t N>
-__global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t steps) {
+__global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t share) {
   constexpr uint32_t E = 16 / sizeof(T), V = N / E, kStep = 64 * N;   // logits of 16 bytes, such loads of a step, logits of a step
   __shared__ uint64_t fresh[4][128], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
   // what hot steps pass from lane to lane (4 more: reads of the logits of several lanes spread over the banks), then the entries of the join
@@ -926,7 +926,7 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   const uint32_t head = min(a.vocab, (uint32_t)((16u - ((uintptr_t)x & 15u)) & 15u) / (uint32_t)sizeof(T));   // logits in front of a 16-byte boundary
   const uint32_t nvec = (a.vocab - head) / E, tail = a.vocab - head - nvec * E;
   const MPK_GLOBAL u32x4* xv = (const MPK_GLOBAL u32x4*)(x + head);
-  const uint32_t v0 = chunk * steps * (kStep / E), v1 = min(nvec, v0 + steps * (kStep / E));
+  const uint32_t v0 = chunk * share, v1 = min(nvec, v0 + share);
   float asked = 0.f;
 
   // The sums count in powers of two from c = log2(e) (m - shift) as rounded, so that an exponent is one fused operation; shift is 0
@@ -1102,15 +1102,18 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
 
 template <typename T>
 static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
-  // a workgroup's share: a whole row where there are rows enough for all compute units, 4096 logits or more
+  constexpr uint32_t E = 16 / sizeof(T);
+  // a workgroup's share, in loads of 16 bytes: a whole row where there are rows enough for all compute units, else 4096 logits or
+  // more, alike for all (filled one after the other, the last one's wavefronts without logits have no bound on the alternatives:
+  // one row of 151936 with 20 12.1 us instead of 11.8)
   if (a.n_rows >= kLogprobManyRows) {
-    rows_logprobs_kernel<T, 1, 16><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, a.vocab / (64u * 16) + 1u);
+    rows_logprobs_kernel<T, 1, 16><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, a.vocab / E);
     return hipGetLastError();
   }
   constexpr uint32_t kRound = 4u * 64u * 16u;   // logits that a workgroup takes at once
   const uint32_t all = (a.vocab + kRound - 1u) / kRound, want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
-  const uint32_t n = std::min(std::min(want, all), kLogprobChunks), steps = 4u * ((all + n - 1u) / n), chunks = (4u * all + steps - 1u) / steps;
-  rows_logprobs_kernel<T, 4, 16><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, steps);
+  const uint32_t n = std::min(std::min(want, all), kLogprobChunks), rounds = (all + n - 1u) / n, chunks = (all + rounds - 1u) / rounds;
+  rows_logprobs_kernel<T, 4, 16><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, (a.vocab / E + chunks - 1u) / chunks);
   return hipGetLastError();
 }
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream) {
