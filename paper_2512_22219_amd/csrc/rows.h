@@ -22,7 +22,7 @@ struct RowSeqs {
   const int32_t* table;       // paged cache: [slot][blocks], else null
   uint32_t page_shift, n_pages, blocks;
   uint32_t n_q, n_kv, head_dim, batch, max_seq;
-  uint32_t *err, *arrivals;
+  uint32_t* err;
 };
 
 struct AppendArgs {

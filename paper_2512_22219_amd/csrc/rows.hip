@@ -98,10 +98,13 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
   *(MPK_GLOBAL u32x4*)p = w;
 }
 
-// A wavefront takes one row and a run of `per_wave` groups of its heads; a group is 64 / LPH heads, a head LPH lanes, a lane 8
-// elements of the head's lower half and the 8 they are rotated with.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t per_wave, uint32_t waves_per_row) {
+// q and k of a head, normed if the model has gains (x gain / sqrt(mean(x^2) + eps)), then pairs (x_i, x_{i + d/2}) turned by the
+// angle position inv_freq[i], which is worked out and reduced to one turn in 64 bits.
+// A wavefront takes one row and G groups of its heads; a group is 64 / LPH heads, a head LPH lanes, a lane 8
+// elements of the head's lower half and the 8 they are rotated with.  Bound by memory: 8192 rows of 64 + 2 x 8 heads of 128, 336 MB
+// read and written, 60 us, 5.6 TB/s (a copy of 1 GiB reaches 5.07: part of this fits the last cache).
+template <typename T, int D, uint32_t G>
+__global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t waves_per_row) {
   constexpr uint32_t LPH = D / 16, HPG = 64 / LPH, HALF = D / 2;
   __shared__ float2 angles[4][HALF];
   const RowSeqs& s = a.s;
@@ -113,6 +116,15 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
   if (seq == 64u) return;
   const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane(q.pos, seq) + row - (uint32_t)__builtin_amdgcn_readlane(q.begin, seq);
   const uint32_t slot = (uint32_t)__builtin_amdgcn_readlane(q.slot, seq);
+  const uint32_t sub = lane & (LPH - 1u), heads = s.n_q + 2u * s.n_kv, e = 8u * sub;
+  const T* x = (const T*)a.qkv + (size_t)row * a.qkv_stride;
+  float lo[G][8], hi[G][8];   // (on their way while the angles are worked out)
+#pragma unroll
+  for (uint32_t g = 0; g < G; ++g) {
+    const uint32_t h = min((part * G + g) * HPG + lane / LPH, heads - 1u);
+    load8(x + (size_t)h * D + e, lo[g]);
+    load8(x + (size_t)h * D + HALF + e, hi[g]);
+  }
   if (lane < HALF) {
     const double two_pi = 6.283185307179586476925286766559;
     double ang = (double)(int32_t)pos * as_global(a.inv_freq)[lane];
@@ -121,30 +133,26 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
     sincos(ang, &sn, &cs);
     angles[wave][lane] = make_float2((float)cs, (float)sn);
   }
-  const uint32_t sub = lane & (LPH - 1u), heads = s.n_q + 2u * s.n_kv, e = 8u * sub;
   float2 cs[8];
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int i = 0; i < 8; ++i) cs[i] = angles[wave][e + i];
-  const T* x = (const T*)a.qkv + (size_t)row * a.qkv_stride;
   size_t at = 0;
   const bool cached = cache_row(s, slot, 0, pos, &at);
   if (!cached && lane == 0 && part == 0) report_rows(s.err, DE_BAD_PAGE, seq, pos);
   const size_t kv_head = s.table ? (size_t)D << s.page_shift : (size_t)D * s.max_seq;
-  for (uint32_t g = 0; g < per_wave; ++g) {
-    const uint32_t h = (part * per_wave + g) * HPG + lane / LPH;
+#pragma unroll
+  for (uint32_t g = 0; g < G; ++g) {
+    const uint32_t h = (part * G + g) * HPG + lane / LPH;
     if (h >= heads) continue;
-    float lo[8], hi[8];
-    load8(x + (size_t)h * D + e, lo);
-    load8(x + (size_t)h * D + HALF + e, hi);
     const bool is_v = h >= s.n_q + s.n_kv, is_q = h < s.n_q;
     if (!is_v) {
       const uint16_t* gain = is_q ? a.q_norm : a.k_norm;
       if (gain) {
         float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(hi[i], hi[i], fmaf(lo[i], lo[i], ss));
+        for (int i = 0; i < 8; ++i) ss = fmaf(hi[g][i], hi[g][i], fmaf(lo[g][i], lo[g][i], ss));
 #pragma unroll
         for (uint32_t o = 1; o < LPH; o *= 2) ss += __shfl_xor(ss, o, 64);
         const float inv = 1.0f / sqrtf(ss * (1.0f / (float)D) + a.eps);
@@ -152,21 +160,21 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
         load8(gain + e, gl);
         load8(gain + HALF + e, gh);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { lo[i] = lo[i] * inv * gl[i]; hi[i] = hi[i] * inv * gh[i]; }
+        for (int i = 0; i < 8; ++i) { lo[g][i] = lo[g][i] * inv * gl[i]; hi[g][i] = hi[g][i] * inv * gh[i]; }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float l = lo[i], u = hi[i];
-        lo[i] = fmaf(l, cs[i].x, -(u * cs[i].y));
-        hi[i] = fmaf(u, cs[i].x, l * cs[i].y);
+        const float l = lo[g][i], u = hi[g][i];
+        lo[g][i] = fmaf(l, cs[i].x, -(u * cs[i].y));
+        hi[g][i] = fmaf(u, cs[i].x, l * cs[i].y);
       }
     }
     uint16_t* to = nullptr;
     if (is_q) to = a.q_out + (size_t)row * a.q_stride + (size_t)h * D;
     else if (cached) to = (is_v ? s.v + at + (size_t)(h - s.n_q - s.n_kv) * kv_head : s.k + at + (size_t)(h - s.n_q) * kv_head);
     if (to) {
-      store8(to + e, lo);
-      store8(to + HALF + e, hi);
+      store8(to + e, lo[g]);
+      store8(to + HALF + e, hi[g]);
     }
   }
 }
@@ -174,9 +182,13 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
 template <typename T, int D>
 static hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
   const uint32_t groups = (a.s.n_q + 2u * a.s.n_kv + 1024u / D - 1u) / (1024u / D);
-  const uint32_t per_wave = a.s.n_rows <= 256u ? 1u : groups, waves_per_row = (groups + per_wave - 1u) / per_wave;
-  const uint64_t blocks = ((uint64_t)a.s.n_rows * waves_per_row + 3u) / 4u;
-  rows_append_kernel<T, D><<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>(a, per_wave, waves_per_row);
+  // A wavefront more a row works out the row's angles once more; a group more a wavefront has fewer of them.  One / two / four groups a
+  // wavefront (32 + 2 x 8 heads of 128, bf16): 256 rows 3.8 / 4.3 / - us, 512 4.7 / 5.1 / -, 1024 7.0 / 6.7 / 7.4, 2048 11.8 / 11.0 / 11.5,
+  // 4096 19.7 / 18.4 / 19.9.
+  const uint32_t per_wave = a.s.n_rows <= 512u ? 1u : 2u, waves_per_row = (groups + per_wave - 1u) / per_wave;
+  const dim3 blocks((uint32_t)(((uint64_t)a.s.n_rows * waves_per_row + 3u) / 4u));
+  if (per_wave == 1u) rows_append_kernel<T, D, 1><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
+  else rows_append_kernel<T, D, 2><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
   return hipGetLastError();
 }
 hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream) {

@@ -1156,7 +1156,6 @@ static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs,
   s->n_q = h.cfg.n_q_heads; s->n_kv = h.cfg.n_kv_heads; s->head_dim = h.cfg.head_dim;
   s->batch = h.cfg.batch; s->max_seq = h.cfg.max_seq;
   s->err = g->d_err;
-  s->arrivals = g->d_arrivals;
   size_t rows = (size_t)(h.opt.kv_batch ? h.opt.kv_batch : h.cfg.batch) * h.cfg.max_seq;   // of one layer and KV head
   if (h.opt.kv_page_size) {
     s->table = g->page_table;
