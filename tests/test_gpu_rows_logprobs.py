@@ -101,6 +101,18 @@ def test_ties_and_orders(kind, rows, vocab):
     _check(vocab, x, tokens, 20)
 
 
+@pytest.mark.parametrize("n_top", [1, 6, 20, 32])
+@pytest.mark.parametrize("rows,vocab,shift", [(1, 151936, 0.0), (3, 60001, -0.5), (90, 60001, -2.0), (300, 30011, 1.0), (2050, 5000, -9.5)])
+def test_many_equal_logits(rows, vocab, shift, n_top):
+    """Logits in steps of a quarter, so that many are equal to the last alternative; the same bits however the call went."""
+    x, tokens = _inputs(rows, vocab, torch.float32, 12, std=0.5)
+    x = ((4 * x).round() / 4 + shift).to(torch.bfloat16)
+    _check(vocab, x, tokens, n_top)
+    first = _call(vocab, x, tokens, n_top)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, _call(vocab, x, tokens, n_top)))
+
+
 @pytest.mark.parametrize("rows,vocab", [(1, 30011), (3, 8000), (2100, 1000)])
 @pytest.mark.parametrize("level", [1e4, 1.0e6, 1.1e6, 3e7, 1e12, 1e30])
 def test_large_logits(level, rows, vocab):
