@@ -206,6 +206,9 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 //   tile by ds_read_b64_tr_b16.
 // K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
+// What bounds it: many rows, the card's power, which takes the clock down to 1.8 GHz (2048 tokens over 14000 cached, 64 heads on 8 of 128,
+// 1.01 TFLOP: 937 us, 1.08 PFLOP/s; a product of 8192^3 reaches 1.15 to 1.20 on such values, 1.71 on zeros).  Few rows, the cache's
+// bytes behind 4.5 us to the first of them and 4 us of the join (8 sequences of up to 4096, 75.7 MB: 20.6 us).
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
@@ -702,14 +705,23 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------ log probabilities
-// One pass over a row.  A wavefront reads N logits a lane and step and keeps, against the largest m that it has seen,
+// One pass over a row.  A wavefront reads 16 logits a lane and step and keeps, against the largest m that it has seen,
 //   s = sum e^(x - m) without one of the largest, t = sum e^(x - m) (x - m)
 // (ln p = x - m - log1p(s): nothing is lost of a token that is all but certain; entropy = log1p(s) - t / (1 + s)), and its
 // best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
 // With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
+// What bounds it: many rows, the vector operations (an unpack, a half of a maximum, a fused product, an exponential at a quarter of
+// the rate, a floor and two sums a logit: 4096 rows of 32000 bf16, 262 MB, 55 to 61 us with 4 alternatives, 52 with none); in fp32 memory
+// (4096 rows with none 90 us, 5.8 TB/s).  One row of 151936, 11.5 us: what waits for what, a fifth of it each the first logits, the
+// first step's alternatives, a run's join, its way to the others and the row's join.
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
-constexpr uint32_t kLogprobWorkgroups = 1024;   // that a call is cut into where its rows are fewer
-constexpr uint32_t kLogprobManyRows = 2048;     // a wavefront a row from here on
+// Workgroups that a call is cut into where its rows are fewer.  512 / 1024 / 1536 with 20 alternatives: 32 rows of 151936 19.2 / 18.2 /
+// 16.9 us, 64 23.2 / 23.7 / 23.2, 200 37.0 / 35.8 / 40.1; 200 of 32000 20.2 / 18.9 / 20.6, 512 23.7 / 25.8 / 32.0.
+constexpr uint32_t kLogprobWorkgroups = 1024;
+// A wavefront a row from here on.  Four / one, 32000 in bf16 with 4 alternatives: 1536 rows 32.5 / 35.1 us, 2048 38.4 / 36.0, 4096
+// 68 / 56; with 20 43 / 52, 51 / 54, 88 / 76.
+constexpr uint32_t kLogprobManyRows = 2048;
+constexpr uint32_t kLogprobLane = 16;   // logits of a lane and step
 static_assert(kLogprobManyRows <= kRowsArrivals, "a counter a row that is cut");
 constexpr uint32_t kNotLast = 0xFFFFFFFFu;
 
@@ -920,10 +932,10 @@ __device__ __forceinline__ bool join_runs(const LogprobArgs& a, uint32_t row, ui
   return true;
 }
 
-// W wavefronts of a workgroup share a run (4, N = 16: a step is what a run has, or 1, N = 16: a whole row each).
-template <typename T, uint32_t W, uint32_t N>
+// W wavefronts of a workgroup share a run: 4, or 1 and the run is a row.
+template <typename T, uint32_t W>
 __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint32_t chunks, uint32_t share) {
-  constexpr uint32_t E = 16 / sizeof(T), V = N / E, kStep = 64 * N;   // logits of 16 bytes, such loads of a step, logits of a step
+  constexpr uint32_t N = kLogprobLane, E = 16 / sizeof(T), V = N / E, kStep = 64 * N;   // logits of 16 bytes, such loads of a step, logits of a step
   __shared__ uint64_t fresh[4][128], sorted[4][MPK_ROWS_MAX_TOP], list[4 * MPK_ROWS_MAX_TOP], first_best[MPK_ROWS_MAX_TOP];
   // what hot steps pass from lane to lane (4 more: reads of the logits of several lanes spread over the banks), then the entries of the join
   __shared__ __align__(16) uint64_t lists[4 * 64 * (N + 4) / 2];
@@ -947,7 +959,9 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   float c = 0.f, shift = 0.f;
   RowSum r = {-INFINITY, 0.f, 0.f};
   Best best;
-  float bound = -INFINITY, limit = -INFINITY;   // the row's alternatives are not below the first; the last of the best (nothing to beat without alternatives but the largest)
+  // What lies at or below `bound` is no alternative of the row; `limit` is that, or the last of the best.  Without alternatives there
+  // is the largest to beat alone.
+  float bound = -INFINITY, limit = -INFINITY;
   u32x4 next[V];
   auto request = [&](uint32_t first) {
 #pragma unroll
@@ -1125,13 +1139,13 @@ static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   // more, alike for all (filled one after the other, the last one's wavefronts without logits have no bound on the alternatives:
   // one row of 151936 with 20 12.1 us instead of 11.8)
   if (a.n_rows >= kLogprobManyRows) {
-    rows_logprobs_kernel<T, 1, 16><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, a.vocab / E);
+    rows_logprobs_kernel<T, 1><<<dim3((a.n_rows + 3u) / 4u), dim3(256), 0, stream>>>(a, 1u, a.vocab / E);
     return hipGetLastError();
   }
-  constexpr uint32_t kRound = 4u * 64u * 16u;   // logits that a workgroup takes at once
+  constexpr uint32_t kRound = 4u * 64u * kLogprobLane;   // logits that a workgroup takes at once
   const uint32_t all = (a.vocab + kRound - 1u) / kRound, want = (kLogprobWorkgroups + a.n_rows - 1u) / a.n_rows;
   const uint32_t n = std::min(std::min(want, all), kLogprobChunks), rounds = (all + n - 1u) / n, chunks = (all + rounds - 1u) / rounds;
-  rows_logprobs_kernel<T, 4, 16><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, (a.vocab / E + chunks - 1u) / chunks);
+  rows_logprobs_kernel<T, 4><<<dim3(a.n_rows * chunks), dim3(256), 0, stream>>>(a, chunks, (a.vocab / E + chunks - 1u) / chunks);
   return hipGetLastError();
 }
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream) {
