@@ -290,6 +290,29 @@ def test_a_cache_whose_offsets_pass_32_bits(page):
         assert ((out[i].view(2, 128).double() - v.mean(0)).abs() <= bound).all()
 
 
+def test_rows_far_apart():
+    """Row strides of 2^31 elements of qkv, queries and outputs: the third row begins past 2^32."""
+    stride = 1 << 31
+    m = RowsModel(n_q=4, n_kv=2, d=64, layers=1, batch=1, max_seq=64)
+
+    def spread(x):
+        far = torch.empty(2 * stride + x.shape[1], dtype=torch.bfloat16, device=m.dev).as_strided(x.shape, (stride, 1))
+        return far.copy_(x)
+
+    x, work = m.normal(3, 8 * 64), workspace()
+    near = torch.empty(3, 256, dtype=torch.bfloat16, device=m.dev), torch.empty(3, 256, dtype=torch.bfloat16, device=m.dev)
+    far = spread(near[0]), spread(near[1])
+    k0, v0, caches = m.k.clone(), m.v.clone(), []
+    for rows, (q, out) in ((x, near), (spread(x), far)):
+        m.k.copy_(k0)
+        m.v.copy_(v0)
+        m.append(0, [0, 3], None, [40], rows, q)
+        m.attend(0, [0, 3], None, [40], q, out, work)
+        m.status()
+        caches.append((m.k.clone(), m.v.clone()))
+    assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(near + caches[0], far + caches[1]))
+
+
 def test_two_graphs_at_once():
     """Each on a stream of its own, with a workspace of its own."""
     case = dict(n_q=8, n_kv=2, d=128, batch=3, layers=1, max_seq=4096, page=0, lens=[1, 70, 3], pos=[4000, 1300, 9], slots=[0, 1, 2],

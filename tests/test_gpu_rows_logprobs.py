@@ -101,6 +101,23 @@ def test_ties_and_orders(kind, rows, vocab):
     _check(vocab, x, tokens, 20)
 
 
+def test_rows_far_apart():
+    """Row strides of 2^31 elements: the third row begins past 2^32."""
+    vocab, stride = 5000, 1 << 31
+    x, tokens = _inputs(3, vocab, torch.bfloat16, 4)
+    far = torch.empty(2 * stride + vocab, dtype=torch.bfloat16, device="cuda").as_strided((3, vocab), (stride, 1))
+    far.copy_(x)
+    for a, b in zip(_call(vocab, x, tokens, 20), _call(vocab, far, tokens, 20)):
+        assert torch.equal(a, b)
+    _check(vocab, far, tokens, 20)
+
+
+def test_a_million_rows():
+    vocab, rows = 64, (1 << 20) + 3
+    x, tokens = _inputs(rows, vocab, torch.bfloat16, 5)
+    _check(vocab, x, tokens, 3)
+
+
 @pytest.mark.parametrize("n_top", [1, 6, 20, 32])
 @pytest.mark.parametrize("rows,vocab,shift", [(1, 151936, 0.0), (3, 60001, -0.5), (90, 60001, -2.0), (300, 30011, 1.0), (2050, 5000, -9.5)])
 def test_many_equal_logits(rows, vocab, shift, n_top):
