@@ -2,6 +2,8 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <mutex>
+#include <vector>
 
 #include "kernels.h"
 
