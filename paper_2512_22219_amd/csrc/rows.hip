@@ -225,8 +225,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t lds_u32 __attribute__((address_space(3)));
 
-// How a call's work is cut: every wavefront works it out for itself from the lanes' sequences (a lane each, 16 at most: one row
-// of a data-parallel-primitive).
+// How a call's work is cut: every wavefront works it out for itself from the lanes' sequences (a lane each, 16 at most: a row of
+// lanes).
 struct Deal {
   uint32_t tiles, chunks, blocks;   // of the lane's sequence: row tiles, runs of blocks that the longest is cut into, blocks of a run
   uint32_t whole, units;            // runs that all tiles have; units, of one KV head
@@ -761,11 +761,12 @@ __device__ __forceinline__ RowSum join_sums(const RowSum& a, uint32_t n) {
   return RowSum{m, wave_sum_dpp(s), wave_sum_dpp(t)};
 }
 
-// The best k of n entries in LDS, in order, into best [k] (empty before).  The whole workgroup calls it: an entry's place is the
-// number of entries above it, eight lanes count an eighth of them each.
-__device__ __forceinline__ void rank_entries(const uint64_t* list, uint32_t n, uint32_t k, uint64_t* best) {
-  for (uint32_t i0 = 0; i0 < n; i0 += 32u) {
-    const uint32_t i = i0 + (threadIdx.x >> 3);
+// The best k of n entries in LDS, in order, into best [k] (empty before).  Called by whole wavefronts, WAVES of them, this one the
+// wave-th: an entry's place is the number of entries above it, eight lanes count an eighth of them each.
+template <uint32_t WAVES>
+__device__ __forceinline__ void rank_entries(uint32_t wave, const uint64_t* list, uint32_t n, uint32_t k, uint64_t* best) {
+  for (uint32_t i0 = 0; i0 < n; i0 += 8u * WAVES) {
+    const uint32_t i = i0 + 8u * wave + ((threadIdx.x & 63u) >> 3);
     const uint64_t mine = i < n ? list[i] : 0;
     uint32_t rank = 0;
 #pragma unroll 4
@@ -903,32 +904,31 @@ __device__ __forceinline__ bool join_runs(const LogprobArgs& a, uint32_t row, ui
   if (n == kNotLast) return false;
   // everything that the runs left, in one round of loads
   constexpr uint32_t kPer = kLogprobChunks * MPK_ROWS_MAX_TOP / 256u;
-  uint64_t e[kPer], nth_best = 0;
+  uint64_t e[kPer];
   const uint32_t nth = min(k, (2u * k + chunks - 1u) / chunks);
 #pragma unroll
   for (uint32_t j = 0; j < kPer; ++j) e[j] = threadIdx.x + 256u * j < chunks * k ? ld_relaxed64(entries + threadIdx.x + 256u * j) : 0;
-  if (threadIdx.x < 64u) {
+  if (threadIdx.x < 64u) {   // (the sums: the first wavefront writes them)
     r = RowSum{-INFINITY, 0.f, 0.f};
     if (lane < chunks) {
-      if (k) nth_best = ld_relaxed64(entries + lane * k + nth - 1u);
       const float2 ms = ld_act2((const float*)(sums + 2u * lane));
       r.m = ms.x; r.s = ms.y; r.t = ld_act((const float*)(sums + 2u * lane + 1u));
     }
     r = join_sums(r, chunks);
+  } else if (k && threadIdx.x < 128u) {   // (beside it)
     // ceil(k / nth) runs have nth entries at or above the one that this many runs' nth entries are not below: k of the row are,
     // and few others where about half of the runs have one
-    if (k) {
-      const uint32_t p = nth_largest((uint32_t)(nth_best >> 32), (k + nth - 1u) / nth);
-      if (lane == 0) least = (uint64_t)p << 32;
-      if (lane < k) best[lane] = 0;
-    }
+    const uint64_t nth_best = lane < chunks ? ld_relaxed64(entries + lane * k + nth - 1u) : 0;
+    const uint32_t p = nth_largest((uint32_t)(nth_best >> 32), (k + nth - 1u) / nth);
+    if (lane == 0) least = (uint64_t)p << 32;
+    if (lane < k) best[lane] = 0;
   }
   __syncthreads();
 #pragma unroll
   for (uint32_t j = 0; j < kPer; ++j)
     if (256u * j < chunks * k && e[j] && e[j] >= least) list[atomicAdd(&n, 1u)] = e[j];   // (in any order: an entry's rank goes by all of them)
   __syncthreads();
-  rank_entries(list, n, k, best);
+  rank_entries<4>(threadIdx.x >> 6, list, n, k, best);
   __syncthreads();
   mine = lane < k ? best[lane] : 0;
   return true;
@@ -1122,11 +1122,11 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
     if (lane < k) list[wave * k + lane] = mine;
     if (wave == 1 && lane < k) first_best[lane] = 0;
     __syncthreads();
+    if (wave == 0) r = join_sums(sums[lane & 3u], 4);   // (who writes them; the others meanwhile)
     if (k) {
-      rank_entries(list, 4u * k, k, first_best);
+      if (wave) rank_entries<3>(wave - 1u, list, 4u * k, k, first_best);
       __syncthreads();
     }
-    r = join_sums(sums[lane & 3u], 4);
     if (lane < k) mine = first_best[lane];
     if (chunks > 1u && !join_runs(a, row, chunk, chunks, r, mine, lists)) return;
     if (wave) return;
