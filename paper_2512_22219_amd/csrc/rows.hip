@@ -864,7 +864,7 @@ struct Best {
       const uint32_t n = min(64u, waiting - at);
       const uint64_t now = lane < n ? fresh[at + lane] : 0;
       uint32_t place_now = 0, place_old = lane;
-#pragma unroll 2
+#pragma unroll 4
       for (uint32_t i = 0; i < n; ++i) {
         const uint64_t e = fresh[at + i];
         place_now += e > now;
