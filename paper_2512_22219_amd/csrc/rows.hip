@@ -319,11 +319,14 @@ __device__ __forceinline__ uint32_t swizzle(uint32_t row) {   // 16-byte piece c
 }
 
 // 1 KB of the wavefront's lanes' 16 bytes each into LDS at `to` (lane after lane).  Assembly text, for the compiler waits for a
-// load into LDS before any later read of LDS that it cannot tell apart; who issues it waits (drain_vmem).
+// load into LDS before any later read of LDS that it cannot tell apart; who issues it waits (drain_vmem).  ONCE: what is read leaves
+// the caches first.
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
   const uint64_t p = (uint64_t)base;
   const u32x4 rsrc = {uniform_u32((uint32_t)p), uniform_u32((uint32_t)(p >> 32) & 0xFFFFu), 0x7FFFFFFFu, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
 }
 
 // The largest of three, a NaN left out.  (fmaxf of results of a matrix instruction costs an operation more each, to quiet NaN.)
@@ -335,7 +338,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 __device__ __forceinline__ uint32_t nonfinite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }   // bit 15 / 31: lower / upper
 
-template <int D, bool PAGED>
+// ONCE: no sequence has more than one tile, so that a unit's keys are its own.
+template <int D, bool PAGED, bool ONCE>
 __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) {
   constexpr uint32_t KS = D / 16, NT = D / 32, CPR = D / 8, RPI = 64 / CPR, IPW = 16 / RPI, ROWB = D * 2, TILE = kBlockKeys * ROWB;
   extern __shared__ __align__(16) unsigned char tiles_lds[];   // K, V of the even blocks, K, V of the odd ones, a flag
@@ -417,8 +421,8 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         const uint32_t j = whole ? jrow[i] : min(r0 + jrow[i], last) - c0;
         const size_t at = PAGED ? (((size_t)pg[i * RPI / 8u] * s.n_kv << s.page_shift) + (c0 & ((1u << s.page_shift) - 1u))) * D : (size_t)c0 * D;
         const uint32_t to = lds0 + buf * 2u * TILE + (wave * IPW + i) * 1024u, off = j * ROWB + voff[i];
-        load_to_lds(kbase + at, off, to);
-        load_to_lds(vbase + at, off, to + TILE);
+        load_to_lds<ONCE>(kbase + at, off, to);
+        load_to_lds<ONCE>(vbase + at, off, to + TILE);
       }
     };
     fetch_pages(b0);
@@ -678,7 +682,8 @@ hipError_t rows_prepare(int device) {
   std::lock_guard<std::mutex> lock(mu);
   if ((size_t)device < done.size() && done[device]) return hipSuccess;
   hipError_t e = hipSuccess;
-  for (const void* fn : {(const void*)rows_attend_kernel<128, false>, (const void*)rows_attend_kernel<128, true>})
+  for (const void* fn : {(const void*)rows_attend_kernel<128, false, false>, (const void*)rows_attend_kernel<128, true, false>,
+                         (const void*)rows_attend_kernel<128, false, true>, (const void*)rows_attend_kernel<128, true, true>})
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_lds(128));
   if (e == hipSuccess) {
     done.resize(std::max(done.size(), (size_t)device + 1u));
@@ -693,7 +698,11 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   // one takes several where there are more)
   const uint64_t tiles = (((uint64_t)a.s.n_rows << lg) / kTileRows + a.s.n_seqs) * a.s.n_kv;
   const uint32_t grid = (uint32_t)std::min<uint64_t>(tiles <= kAttendSlots / 2u ? kAttendSlots : tiles + (tiles <= 2u * kAttendSlots ? kAttendSlots : kAttendSlots / 4u), 1u << 20);
-  rows_attend_kernel<D, PAGED><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+  // Rows of one tile at most: keys that are kept would only drive out others from the caches.  (Kept / not, 10 layers' caches in turn: 8 x 1
+  // token over 512 to 4096 24.7 / 22.8 us, 16 x 1 over 4000 52.6 / 47.9; one call's cache, which stays in the last cache, 21.9 / 21.9.  Several
+  // tiles a sequence, 16 ragged prompts: 147 / 159.)
+  if (a.s.n_rows << lg <= kTileRows) rows_attend_kernel<D, PAGED, true><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+  else rows_attend_kernel<D, PAGED, false><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
   rows_attend_join_kernel<D><<<dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
