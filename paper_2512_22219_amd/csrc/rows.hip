@@ -263,12 +263,12 @@ __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d) {
 __device__ __forceinline__ uint32_t first_tile_of_run(uint32_t k, uint32_t blocks, uint32_t pos, uint32_t lg) {
   return ((k * blocks * kBlockKeys - pos) << lg) / kTileRows;
 }
-template <int D>
+template <int D, bool ONCE>   // ONCE: no sequence has more than one tile
 __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, uint32_t lg) {
   const uint32_t lane = threadIdx.x & 63u, T = (uint32_t)(q.end - q.begin), rows = T << lg;
   auto add = [](auto x, auto y) { return x + y; };
   Deal d;
-  d.tiles = (rows + kTileRows - 1u) / kTileRows;
+  d.tiles = ONCE ? min(T, 1u) : (rows + kTileRows - 1u) / kTileRows;
   const uint32_t nb = T ? ((uint32_t)q.pos + T + kBlockKeys - 1u) / kBlockKeys : 0u;
   const uint32_t few = row16_reduce(d.tiles, add) * s.n_kv;
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
@@ -291,9 +291,12 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   d.blocks = max(1u, quotient(nb + d.chunks - 1u, d.chunks));
   d.chunks = T ? quotient(nb + d.blocks - 1u, d.blocks) : 0u;
   // a run whose first key lies behind the sequence's first new row is not every tile's
-  d.whole = T ? min(d.chunks, quotient((uint32_t)q.pos / kBlockKeys, d.blocks) + 1u) : 0u;
-  d.units = d.tiles * d.whole;
-  for (uint32_t k = d.whole; k < d.chunks; ++k) d.units += d.tiles - first_tile_of_run(k, d.blocks, (uint32_t)q.pos, lg);
+  if constexpr (ONCE) d.whole = d.units = d.chunks;
+  else {
+    d.whole = T ? min(d.chunks, quotient((uint32_t)q.pos / kBlockKeys, d.blocks) + 1u) : 0u;
+    d.units = d.tiles * d.whole;
+    for (uint32_t k = d.whole; k < d.chunks; ++k) d.units += d.tiles - first_tile_of_run(k, d.blocks, (uint32_t)q.pos, lg);
+  }
   const uint32_t units = d.units * s.n_kv, floats = d.chunks > 1u ? d.tiles * d.chunks * s.n_kv * held * (D + 2u) : 0u;
   d.total = row16_reduce(units, add);
   d.part = row16_before(floats);
@@ -349,7 +352,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
   __builtin_amdgcn_s_setprio(3);   // (until the unit's first requests are out: 8 x 1 token 20.3 / 19.6 us)
   const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
-  const Deal d = deal_units<D>(s, q, lg);
+  const Deal d = deal_units<D, ONCE>(s, q, lg);
   const uint32_t total = uniform_u32(d.total);
   if (blockIdx.x == 0 && threadIdx.x < kMaxRowSeqs) {   // what the join needs of it
     MPK_GLOBAL u32x4* to = as_global((u32x4*)a.work) + 2u * threadIdx.x;
@@ -368,7 +371,8 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     const uint32_t tiles = __builtin_amdgcn_readlane(d.tiles, seq), whole = __builtin_amdgcn_readlane(d.whole, seq);
     const uint32_t v = u - __builtin_amdgcn_readlane(d.first_unit, seq), kvh = v % s.n_kv;
     uint32_t w = v / s.n_kv, chunk = w / tiles;
-    if (chunk < whole) w -= chunk * tiles;
+    if (ONCE) { chunk = w; w = 0; }
+    else if (chunk < whole) w -= chunk * tiles;
     else {
       w -= whole * tiles;
       for (chunk = whole;; ++chunk) {
@@ -377,7 +381,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         w -= n;
       }
     }
-    const uint32_t tile = tiles - 1u - w;
+    const uint32_t tile = ONCE ? 0u : tiles - 1u - w;
     const uint32_t nb = tile_blocks(pos0, T, tile, lg), b0 = chunk * per, b1 = min(nb, b0 + per);
     const uint32_t rows = T << lg, last = pos0 + T - 1u;   // the sequence's last row in the cache
     const uint32_t w0 = tile * kTileRows + wave * 32u;   // the wavefront's rows: none behind `rows`
