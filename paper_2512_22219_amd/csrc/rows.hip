@@ -727,7 +727,7 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 // With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
 // What bounds it: many rows, the vector operations (an unpack, a half of a maximum, a fused product, an exponential at a quarter of
 // the rate, a floor and two sums a logit: 4096 rows of 32000 bf16, 262 MB, 55 to 61 us with 4 alternatives, 52 with none); in fp32 memory
-// (4096 rows with none 90 us, 5.8 TB/s).  One row of 151936, 11.5 us: what waits for what, a fifth of it each the first logits, the
+// (4096 rows with 5 83 us, 6.3 TB/s).  One row of 151936 with 20, 11 us: what waits for what, a fifth of it each the first logits, the
 // first step's alternatives, a run's join, its way to the others and the row's join.
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
 // Workgroups that a call is cut into where its rows are fewer.  512 / 1024 / 1536 with 20 alternatives: 32 rows of 151936 19.2 / 18.2 /
@@ -977,10 +977,11 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
   // What lies at or below `bound` is no alternative of the row; `limit` is that, or the last of the best.  Without alternatives there
   // is the largest to beat alone.
   float bound = -INFINITY, limit = -INFINITY;
+  // Read once, so not to be kept (kept / not: 1024 rows of 151936 108 / 97 us, 4096 of 32000 91 / 83, in bf16 58.4 / 58.0; few rows alike).
   u32x4 next[V];
   auto request = [&](uint32_t first) {
 #pragma unroll
-    for (uint32_t j = 0; j < V; ++j) next[j] = xv[min(first + j * 64u + lane, v1 - 1u)];
+    for (uint32_t j = 0; j < V; ++j) next[j] = __builtin_nontemporal_load(xv + min(first + j * 64u + lane, v1 - 1u));
   };
   uint32_t at = v0 + part_of * (kStep / E);
   if (at < v1) request(at);
