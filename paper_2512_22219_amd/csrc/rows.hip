@@ -726,7 +726,7 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 // best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
 // With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
 // What bounds it: many rows, the vector operations (an unpack, a half of a maximum, a fused product, an exponential at a quarter of
-// the rate, a floor and two sums a logit: 4096 rows of 32000 bf16, 262 MB, 55 to 61 us with 4 alternatives, 52 with none); in fp32 memory
+// the rate, a floor and two sums a logit: 4096 rows of 32000 bf16, 262 MB, 53 to 58 us with 4 alternatives, 50 with none); in fp32 memory
 // (4096 rows with 5 83 us, 6.3 TB/s).  One row of 151936 with 20, 11 us: what waits for what, a fifth of it each the first logits, the
 // first step's alternatives, a run's join, its way to the others and the row's join.
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
