@@ -1,5 +1,6 @@
 """mpk_rows_logprobs on the GPU against 64-bit results."""
 import math
+import random
 
 import pytest
 import torch
@@ -99,6 +100,23 @@ def test_ties_and_orders(kind, rows, vocab):
         assert torch.equal(ids[:, 1:], torch.arange(19, device="cuda", dtype=torch.int32).expand(rows, 19))
         return
     _check(vocab, x, tokens, 20)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_drawn_rows(seed):
+    rng = random.Random(seed)
+    vocab = rng.choice([rng.randint(1, 300), rng.randint(300, 9000), rng.randint(9000, 160000)])
+    rows = rng.choice([1, 2, rng.randint(3, 60), max(1, min(rng.randint(60, 3000), (1 << 25) // vocab))])
+    dtype, pad, n_top = rng.choice([torch.float32, torch.bfloat16]), rng.choice([0, 0, 1, 5, 64]), min(vocab, rng.choice([0, 1, 3, 20, 32]))
+    x, tokens = _inputs(rows, vocab, dtype, seed, std=rng.choice([0.01, 3.0, 40.0]), pad=pad)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    if rng.random() < 0.4:   # tokens ruled out, up to all but two in a hundred; the first token stays
+        out = torch.rand(rows, vocab, generator=gen, device="cuda") < rng.choice([0.1, 0.9, 0.98])
+        out[:, 0] = False
+        x.masked_fill_(out, -math.inf)
+    if rng.random() < 0.3:
+        tokens[torch.rand(rows, generator=gen, device="cuda") < 0.5] = -1
+    _check(vocab, x, tokens, n_top)
 
 
 def test_rows_far_apart():
