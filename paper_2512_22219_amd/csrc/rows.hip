@@ -216,6 +216,9 @@ constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
 constexpr float kAttendShare = 1.8e-4f;      // ... and a row's partial result
 constexpr uint32_t kJoinWorkgroups = 1024;
+// Rows and heads, up to as many as there are compute units, that get a workgroup each in the join (a wavefront / a workgroup each: 1 token
+// over 30000, 32 heads of 128, 30.6 / 26.0 us; 5 over 30000 of 64 20.1 / 17.9; 8 over 8000, 256 of them, 18.4 / 17.0; 512 18.8 / 19.3; 1024 14.7 / 16.7).
+constexpr uint32_t kJoinFewItems = 256;
 constexpr uint32_t kAttendHeader = 1024;   // floats of the workspace in front of the partial results
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
 
@@ -609,10 +612,12 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
   }
 }
 
-// Joins the partial results of a row whose tile was cut into runs, in their order: a wavefront per row and query head.
-template <int D>
+// Joins the partial results of a row whose tile was cut into runs, in their order: W wavefronts per row and query head, every W-th
+// run each.
+template <int D, uint32_t W>
 __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uint32_t lg) {
-  __shared__ float weight[4][kAttendMostChunks + 16u];
+  __shared__ float parts[4][D];
+  __shared__ float weight[4][kAttendMostChunks + 16u * W];
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
   SeqLanes q = {0, 0, -1, 0};
@@ -623,7 +628,8 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
     seq_chunks = x[3]; blocks = y[0]; seq_part = y[1];
   }
   if (!__ballot(seq_chunks > 1u)) return;
-  for (uint64_t item = blockIdx.x * 4u + wave; item < (uint64_t)s.n_rows * s.n_q; item += gridDim.x * 4u) {
+  const uint32_t mine = W == 1 ? 0u : wave;   // first run
+  for (uint64_t item = W == 1 ? blockIdx.x * 4u + wave : blockIdx.x; item < (uint64_t)s.n_rows * s.n_q; item += gridDim.x * (4u / W)) {
   const uint32_t row = (uint32_t)(item / s.n_q), head = (uint32_t)(item - (uint64_t)row * s.n_q);
   const uint32_t seq = seq_of_row(q, row);
   if (seq == 64u) continue;
@@ -645,7 +651,7 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
 #pragma unroll
     for (uint32_t j = 0; j < 16; ++j)
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(c + j, n - 1u) * stride + e];
+      for (int e = 0; e < D / 64; ++e) v[j][e] = as_global(p)[min(mine + W * (c + j), n - 1u) * stride + e];
   };
 #pragma unroll
   for (uint32_t i = 0; i < kAttendMostChunks / 64; ++i) {
@@ -667,10 +673,21 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
 #pragma unroll
     for (uint32_t j = 0; j < 16; ++j)
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) o[e] = c + j < n ? fmaf(v[j][e], weight[wave][c + j], o[e]) : o[e];
+      for (int e = 0; e < D / 64; ++e) o[e] = mine + W * (c + j) < n ? fmaf(v[j][e], weight[wave][mine + W * (c + j)], o[e]) : o[e];
     c += 16u;
-    if (c >= n) break;
+    if (mine + W * c >= n) break;
     request(c);
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) parts[wave][(D / 64) * lane + e] = o[e];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const float* q = &parts[0][(D / 64) * lane + e];
+      o[e] = (q[0] + q[D]) + (q[2 * D] + q[3 * D]);
+    }
   }
   const float inv = 1.0f / l;
   uint16_t* to = a.out + (size_t)row * a.out_stride + (size_t)head * D + (D / 64) * lane;
@@ -709,7 +726,9 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   else rows_attend_kernel<D, PAGED, false><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
-  rows_attend_join_kernel<D><<<dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.s.n_rows * a.s.n_q + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
+  const uint64_t items = (uint64_t)a.s.n_rows * a.s.n_q;
+  if (items <= kJoinFewItems) rows_attend_join_kernel<D, 4><<<dim3((uint32_t)items), dim3(256), 0, stream>>>(a, lg);
+  else rows_attend_join_kernel<D, 1><<<dim3((uint32_t)std::min<uint64_t>((items + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
   return hipGetLastError();
 }
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
