@@ -221,6 +221,10 @@ constexpr uint32_t kJoinWorkgroups = 1024;
 constexpr uint32_t kJoinFewItems = 256;
 constexpr uint32_t kAttendHeader = 1024;   // floats of the workspace in front of the partial results
 constexpr uint32_t kAttendSlots = 512;   // workgroups that run at once: two a compute unit
+// Calls of one tile a sequence wait for memory, and heads of 64 have room for three a compute unit (two / three: 16 x 1 token over 4000
+// 29.6 / 26.6 us, over 12000 72.1 / 66.9, 8 x 1 over 512 to 4096 14.5 / 13.5; four: 26.7, 67.3, 13.7, but 5 over 30000 18.2 / 18.3 / 19.0).
+constexpr uint32_t attend_slots(uint32_t D, bool once) { return D == 64u && once ? 768u : kAttendSlots; }
+constexpr uint32_t kAttendFewChunks = 64;   // runs of such a tile at most, what a workgroup of the join reads at once (5 over 30000, 87 / 59 runs: 19.5 / 18.3)
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -270,23 +274,28 @@ template <int D, bool ONCE>   // ONCE: no sequence has more than one tile
 __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, uint32_t lg) {
   const uint32_t lane = threadIdx.x & 63u, T = (uint32_t)(q.end - q.begin), rows = T << lg;
   auto add = [](auto x, auto y) { return x + y; };
+  constexpr uint32_t kSlots = attend_slots(D, ONCE);
   Deal d;
   d.tiles = ONCE ? min(T, 1u) : (rows + kTileRows - 1u) / kTileRows;
   const uint32_t nb = T ? ((uint32_t)q.pos + T + kBlockKeys - 1u) / kBlockKeys : 0u;
   const uint32_t few = row16_reduce(d.tiles, add) * s.n_kv;
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
   // few tiles: at most as many units as run at once, all about as long (in 32 bits; no sequence has 2^22 blocks)
-  uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kAttendSlots / 2u ? kAttendSlots - few : kAttendSlots)));
+  uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kSlots / 2u ? kSlots - few : kSlots)));
   // A run more is a partial result more of every tile, written and read: in blocks' time `share`, with all tiles of the call; and the
   // first cut is a second kernel.  So a run is no shorter than the square root that has blocks and partial results cost the same,
-  // and a tile is cut only where that saves more than it costs.  (Cut into as many runs as run at once / as here: 512 tokens 25.6 /
+  // and a tile is cut only where that saves more than it costs.  Where a sequence has one tile at most and all run at once, the kernel
+  // is not counted if another sequence needs it (counted / not: 8 x 1 token over 512 to 4096 21.8 / 19.8 us, heads of 64 17.2 / 14.5; with
+  // several tiles a sequence 4 x 200 to 300 over 1000 to 3000 83 / 88).  (Cut into as many runs as run at once / as here: 512 tokens 25.6 /
   // 17.6 us, eight times 200 over 300 51 / 24; tiles of up to 22 blocks never cut / as here: 64 tokens over 1000 27.6 / 15.3.)
   const uint32_t held = min(rows, kTileRows);
   const float share = (float)few * (float)held * kAttendShare;
   c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
+  if (ONCE) c = max(c, (nb + kAttendFewChunks - 1u) / kAttendFewChunks);
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
     d.chunks = quotient(nb + c - 1u, c);
-    if ((float)nb < (float)c + (float)kAttendJoinBlocks + share * (float)d.chunks) d.chunks = 1u;
+    const float saved = (float)nb - (float)c - share * (float)d.chunks;
+    if (saved < (ONCE && __any(saved >= (float)kAttendJoinBlocks) ? 0.f : (float)kAttendJoinBlocks)) d.chunks = 1u;
     const bool cut = T && d.chunks > 1u;
     const float need = cut ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(held * (D + 2u)) : 0.f;
     if (uniform_f32(row16_reduce(need, add)) <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u) && __all(d.chunks <= kAttendMostChunks)) break;
@@ -304,7 +313,7 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   d.total = row16_reduce(units, add);
   d.part = row16_before(floats);
   d.first_unit = row16_before(units);
-  if (uniform_u32(d.total) > kAttendSlots) {   // not all at once: the sequences with more blocks first
+  if (uniform_u32(d.total) > kSlots) {   // not all at once: the sequences with more blocks first
     d.first_unit = 0;
     for (uint32_t i = 0; i < s.n_seqs; ++i) {
       const uint32_t onb = __builtin_amdgcn_readlane(nb, i), ou = __builtin_amdgcn_readlane(units, i);
@@ -722,7 +731,10 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   // Rows of one tile at most: keys that are kept would only drive out others from the caches.  (Kept / not, 10 layers' caches in turn: 8 x 1
   // token over 512 to 4096 24.7 / 22.8 us, 16 x 1 over 4000 52.6 / 47.9; one call's cache, which stays in the last cache, 21.9 / 21.9.  Several
   // tiles a sequence, 16 ragged prompts: 147 / 159.)
-  if (a.s.n_rows << lg <= kTileRows) rows_attend_kernel<D, PAGED, true><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+  if (a.s.n_rows << lg <= kTileRows) {
+    const uint32_t runs = std::min(kAttendFewChunks, a.s.max_seq / (kAttendMinBlocks * kBlockKeys) + 1u);
+    rows_attend_kernel<D, PAGED, true><<<dim3(std::min(attend_slots(D, true), a.s.n_seqs * a.s.n_kv * runs)), dim3(256), attend_lds(D), stream>>>(a, lg);
+  }
   else rows_attend_kernel<D, PAGED, false><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
