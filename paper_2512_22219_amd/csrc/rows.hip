@@ -282,6 +282,11 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   const float work = row16_reduce(T ? (float)d.tiles * (float)(((uint32_t)q.pos + T / 2u) / kBlockKeys + 1u) : 0.f, add) * (float)s.n_kv;
   // few tiles: at most as many units as run at once, all about as long (in 32 bits; no sequence has 2^22 blocks)
   uint32_t c = 1u + (uint32_t)(uniform_f32(work) * __builtin_amdgcn_rcpf((float)(few <= kSlots / 2u ? kSlots - few : kSlots)));
+  // (That counts a whole run for the last of a tile.  As it is / shorter where that still fits: 4 x 1 token over 3000 15.9 / 15.3 us, 16 x 1 over 1000
+  // 18.7 / 17.6, 8 x 1 over 512 to 4096 19.8 / 19.4.)
+  if (ONCE && uniform_u32(few) <= kSlots / 2u && c > 1u) {
+    if (uniform_u32(row16_reduce(d.tiles * quotient(nb + c - 2u, c - 1u), add)) * s.n_kv <= kSlots) c -= 1u;
+  }
   // A run more is a partial result more of every tile, written and read: in blocks' time `share`, with all tiles of the call; and the
   // first cut is a second kernel.  So a run is no shorter than the square root that has blocks and partial results cost the same,
   // and a tile is cut only where that saves more than it costs.  Where a sequence has one tile at most and all run at once, the kernel
