@@ -210,7 +210,7 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
 // What bounds it: many rows, the card's power, which takes the clock down to 1.8 GHz (2048 tokens over 14000 cached, 64 heads on 8 of 128,
 // 1.01 TFLOP: 937 us, 1.08 PFLOP/s; a product of 8192^3 reaches 1.15 to 1.20 on such values, 1.71 on zeros).  Few rows, the cache's
-// bytes behind 4.5 us to the first of them and 4 us of the join (8 sequences of up to 4096, 75.7 MB: 20.6 us).
+// bytes behind 4.5 us to the first of them and 4 us of the join (8 sequences of up to 4096, 75.7 MB: 19.3 us).
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
