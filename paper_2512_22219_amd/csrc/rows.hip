@@ -349,12 +349,9 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint
   else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
 }
 
-// The largest of three, a NaN left out.  (fmaxf of results of a matrix instruction costs an operation more each, to quiet NaN.)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
+// The largest of three, a NaN left out; one operation, v_max3_f32.  Not as assembly text: the compiler puts the wait states between a
+// matrix instruction and the first reader of its results only where it knows the reader.
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 __device__ __forceinline__ uint32_t nonfinite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }   // bit 15 / 31: lower / upper
 
@@ -1054,10 +1051,9 @@ __global__ void __launch_bounds__(256) rows_logprobs_kernel(LogprobArgs a, uint3
       }
       if (edges && lane < head + tail) y[0] = logit_at(x, lane < head ? lane : a.vocab - tail + (lane - head));
     }
-    float mx = max3(y[0], y[1], y[2]);
+    float mx = -INFINITY;
 #pragma unroll
-    for (uint32_t j = 3; j < N - 1u; j += 2) mx = max3(mx, y[j], y[j + 1]);
-    mx = max3(mx, y[N - 1u], y[N - 1u]);
+    for (uint32_t j = 0; j < N; j += 2) mx = max3(mx, y[j], y[j + 1]);
     if (W > 1 && k) {
       // No less than k logits of the row are at or above the least of the wavefronts' bounds, so what lies below is no answer (an
       // equal logit may be, hence the number below).  It is never above this wavefront's own largest.  The first step's bounds
