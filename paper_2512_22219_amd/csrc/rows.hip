@@ -339,15 +339,20 @@ __device__ __forceinline__ uint32_t swizzle(uint32_t row) {   // 16-byte piece c
 }
 
 // 1 KB of the wavefront's lanes' 16 bytes each into LDS at `to` (lane after lane).  Assembly text, for the compiler waits for a
-// load into LDS before any later read of LDS that it cannot tell apart; who issues it waits (drain_vmem).  ONCE: what is read leaves
-// the caches first.
+// load into LDS before any later read of LDS that it cannot tell apart; who issues it waits (drain_vmem).  The text has the wait states
+// that the compiler does not insert for it: five behind a vector operation that wrote the scalar registers (one would do for m0);
+// m0 is named as lost, for the compiler joins writes of m0 across what it takes to leave it (the warning: m0 is not its to preserve).
+// ONCE: what is read leaves the caches first.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
   const uint64_t p = (uint64_t)base;
   const u32x4 rsrc = {uniform_u32((uint32_t)p), uniform_u32((uint32_t)(p >> 32) & 0xFFFFu), 0x7FFFFFFFu, 0x00020000u};
-  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform_u32(to)), "v"(off), "s"(rsrc) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // The largest of three, a NaN left out; one operation, v_max3_f32.  Not as assembly text: the compiler puts the wait states between a
 // matrix instruction and the first reader of its results only where it knows the reader.

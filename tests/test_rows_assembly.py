@@ -76,3 +76,25 @@ def test_results_of_matrix_instructions_are_waited_for_on_every_path(kernels):
                 if op not in ("s_branch", "s_endpgm"):
                     todo.append((i + 1, after))
     assert checked
+
+
+def test_loads_into_lds_have_their_wait_states(kernels):
+    """A load into LDS is assembly text: one wait state behind the write of m0, five behind a vector operation's of a scalar
+    register that the load reads.  The text has them, whatever the compiler puts in front of it."""
+    checked = 0
+    for name, lines in kernels.items():
+        for text in _texts(lines):
+            for i, line in enumerate(text):
+                if not line.startswith("buffer_load"):
+                    continue
+                checked += 1
+                states = [(int(t.split()[1]) + 1 if t.startswith("s_nop") else 1) for t in text[:i]]
+                assert text[0].startswith("s_mov_b32 m0") and sum(states) >= 5 and sum(states[1:]) >= 1, (name, text)
+    assert checked
+
+
+def test_text_that_writes_m0_says_so():
+    with open(next(s for s in B.SOURCES if os.path.basename(s) == "rows.hip")) as f:
+        texts = re.findall(r"\basm\b.*?;\n", f.read(), re.S)
+    wrote = [t for t in texts if re.search(r"s_mov_b32 m0", t)]
+    assert wrote and all(re.search(r':\s*"memory", "m0"\)', t) for t in wrote)
