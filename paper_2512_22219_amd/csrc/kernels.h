@@ -228,7 +228,7 @@ __device__ __forceinline__ void debug_jitter(const StepArgs& a, uint32_t task_in
   __syncthreads();
 }
 
-enum DevErr : uint32_t { DE_NONE = 0, DE_TIMEOUT = 1, DE_BAD_POSITION = 2, DE_BAD_TOKEN = 3, DE_BAD_META = 4, DE_BAD_PAGE = 5, DE_BAD_ROWS = 6, DE_BAD_SLOT = 7 };
+enum DevErr : uint32_t { DE_NONE = 0, DE_TIMEOUT = 1, DE_BAD_POSITION = 2, DE_BAD_TOKEN = 3, DE_BAD_META = 4, DE_BAD_PAGE = 5, DE_BAD_ROWS = 6, DE_BAD_SLOT = 7, DE_BAD_ROW_TOKEN = 8 };
 
 // ------------------------------------------------------------------------------ device helpers
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }

@@ -859,7 +859,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, uint32_t row, co
       const int32_t t = as_global(a.tokens)[row];
       float lp = nan;
       if (t == -1) lp = 0.f;
-      else if (t < 0 || (uint32_t)t >= a.vocab) report_rows(a.err, DE_BAD_TOKEN, row, (uint32_t)t);
+      else if (t < 0 || (uint32_t)t >= a.vocab) report_rows(a.err, DE_BAD_ROW_TOKEN, row, (uint32_t)t);
       else if (!none) lp = asked - r.m - norm;
       as_global(a.logprobs)[row] = lp;
     }

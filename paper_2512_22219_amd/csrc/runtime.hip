@@ -707,6 +707,9 @@ extern "C" mpk_status mpk_graph_status(mpk_graph* g) {
     case DE_BAD_ROWS:
       set_error("row_begin does not ascend within the call's rows: sequence %u ends at %d", err[2], (int)err[3]);
       return MPK_ERR_DEVICE;
+    case DE_BAD_ROW_TOKEN:
+      set_error("sequence %u has token %d outside [-1, vocab): row %u of a call of mpk_rows_logprobs, where each row is a sequence of its own", err[2], (int)err[3], err[2]);
+      return MPK_ERR_DEVICE;
     case DE_BAD_SLOT:
       set_error("sequence %u has slot %d, outside [0, batch) or an earlier sequence's", err[2], (int)err[3]);
       return MPK_ERR_DEVICE;

@@ -201,6 +201,19 @@ def test_tokens_out_of_range_are_reported():
     _check(1000, x, tokens, 3)
 
 
+@pytest.mark.parametrize("rows,vocab", [(4, 1000), (3, 30011), (2100, 300)])
+def test_a_token_out_of_range_is_reported_with_its_row(rows, vocab):
+    x, tokens = _inputs(rows, vocab, torch.float32, 4)
+    tokens[rows - 1] = -2
+    _call(vocab, x, tokens, 3)
+    with pytest.raises(M.MpkError, match=rf"token -2 outside \[-1, vocab\).*row {rows - 1} of a call") as e:
+        _graph(vocab).status()
+    assert e.value.status == M.MPK_ERR_DEVICE
+    _graph(vocab).reset()
+    tokens[rows - 1] = -1
+    _check(vocab, x, tokens, 3)
+
+
 @pytest.mark.parametrize("rows,vocab", [(2, 151936), (700, 3001)])
 def test_parts_of_the_answer_alone(rows, vocab):
     x, tokens = _inputs(rows, vocab, torch.bfloat16, 5)
