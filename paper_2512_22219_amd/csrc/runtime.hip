@@ -1137,6 +1137,10 @@ static mpk_status rows_work(const void* workspace) {
   if (!workspace || (uintptr_t)workspace % 16) { set_error("workspace is NULL or not 16-byte aligned"); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
 }
+static mpk_status rows_words(const char* name, const void* p) {   // (NULL where the call may leave it out)
+  if ((uintptr_t)p % 4) { set_error("%s is not aligned to its elements", name); return MPK_ERR_INVALID_ARG; }
+  return MPK_OK;
+}
 constexpr uint32_t kRowsMost = 1u << 24;   // rows of a call
 constexpr uint32_t kRowsMostSeq = 1u << 28;   // max_seq of the graph
 static mpk_status rows_count(uint32_t n_rows) {
@@ -1151,7 +1155,10 @@ static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs,
   if (layer >= h.cfg.n_layers) { set_error("layer %u, the model has %u", layer, h.cfg.n_layers); return MPK_ERR_INVALID_ARG; }
   if (n_seqs == 0 || n_seqs > std::min(h.cfg.batch, kMaxRowSeqs)) { set_error("n_seqs %u is outside 1..%u, the graph's batch", n_seqs, h.cfg.batch); return MPK_ERR_INVALID_ARG; }
   if (h.cfg.max_seq > kRowsMostSeq) { set_error("max_seq %u is above %u", h.cfg.max_seq, kRowsMostSeq); return MPK_ERR_UNSUPPORTED; }
-  const mpk_status st = rows_count(n_rows);
+  mpk_status st = rows_count(n_rows);
+  if (st == MPK_OK) st = rows_words("row_begin", row_begin);
+  if (st == MPK_OK) st = rows_words("slots", slots);
+  if (st == MPK_OK) st = rows_words("positions", positions);
   if (st != MPK_OK) return st;
   *s = RowSeqs{};
   s->row_begin = row_begin; s->slots = slots; s->positions = positions;
@@ -1233,6 +1240,8 @@ extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const voi
   if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
   if (!tokens != !logprobs) { set_error("tokens and logprobs: both or neither"); return MPK_ERR_INVALID_ARG; }
   if (n_top && (!top_tokens || !top_logprobs)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_words("tokens", tokens)) != MPK_OK || (st = rows_words("logprobs", logprobs)) != MPK_OK || (st = rows_words("entropy", entropy)) != MPK_OK) return st;
+  if (n_top && ((st = rows_words("top_tokens", top_tokens)) != MPK_OK || (st = rows_words("top_logprobs", top_logprobs)) != MPK_OK)) return st;
   if ((st = rows_work(workspace)) != MPK_OK) return st;
   if ((st = rows_runnable(g)) != MPK_OK || (!tokens && !entropy && !n_top)) return st;
   LogprobArgs a{};

@@ -53,6 +53,18 @@ def test_logprobs(model, change, match):
     _refused(model.graph.rows_logprobs, *dict(LOGITS, **change).values(), match=match)
 
 
+@pytest.mark.parametrize("off", [1, 2])
+@pytest.mark.parametrize("call,args,name,says", [
+    ("rows_append", APPEND, "begin", "row_begin"), ("rows_append", APPEND, "slots", "slots"), ("rows_append", APPEND, "positions", "positions"),
+    ("rows_attend", ATTEND, "begin", "row_begin"), ("rows_attend", ATTEND, "slots", "slots"), ("rows_attend", ATTEND, "positions", "positions"),
+    ("rows_logprobs", LOGITS, "tokens", "tokens"), ("rows_logprobs", LOGITS, "logprobs", "logprobs"), ("rows_logprobs", LOGITS, "entropy", "entropy"),
+    ("rows_logprobs", LOGITS, "top_tokens", "top_tokens"), ("rows_logprobs", LOGITS, "top_logprobs", "top_logprobs")])
+def test_lists_and_results_off_their_elements(model, call, args, name, says, off):
+    assert name in args
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + off}).values(), match=f"^.*{says} is not aligned")
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + 4}).values(), match="host_only")
+
+
 def test_fewer_tokens_than_alternatives():
     g = RowsModel(vocab=8, host_only=True).graph
     _refused(g.rows_logprobs, *dict(LOGITS, n_top=9).values(), match="n_top 9")
