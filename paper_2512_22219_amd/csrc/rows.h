@@ -9,7 +9,7 @@ namespace mpk {
 constexpr uint32_t kMaxRowSeqs = 16;   // sequences of a call: at most a graph's batch
 // A graph's counters of the workgroups that have finished their part of a row, zero between calls; each on a line of its own (16
 // rows of 32 parts: 11.0 us, counted on one line 15.4).
-constexpr uint32_t kRowsArrivals = 2048, kArrivalStride = 32;
+constexpr uint32_t kRowsArrivals = 1024, kArrivalStride = 32;
 
 // The sequences of a call, on a layer's cache.
 struct RowSeqs {

@@ -775,7 +775,7 @@ constexpr uint32_t kLogprobWorkgroups = 1024;
 // 68 / 56; with 20 43 / 52, 51 / 54, 88 / 76.
 constexpr uint32_t kLogprobManyRows = 2048;
 constexpr uint32_t kLogprobLane = 16;   // logits of a lane and step
-static_assert(kLogprobManyRows <= kRowsArrivals, "a counter a row that is cut");
+static_assert(kLogprobWorkgroups == kRowsArrivals, "a counter for each row of a call that cuts its rows: there are fewer of them than this");
 constexpr uint32_t kNotLast = 0xFFFFFFFFu;
 
 // A logit and its token as one number: larger logits first, of equal ones the lower token.  0: none.

@@ -77,6 +77,15 @@ def test_random_rows(rows, vocab, n_top, pad, dtype):
     _check(vocab, x, tokens, n_top)
 
 
+@pytest.mark.parametrize("rows", [1023, 1024, 1025, 2047, 2048])
+def test_as_many_rows_as_are_cut_and_more(rows):
+    """Rows of a call are cut into runs up to 1023 of them; each has a counter of its own, twice in a row."""
+    x, tokens = _inputs(rows, 8193, torch.float32, rows)
+    _check(8193, x, tokens, 8)
+    first, second = _call(8193, x, tokens, 8), _call(8193, x, tokens, 8)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("offset", [1, 3])
 def test_rows_at_any_address(offset, dtype):
