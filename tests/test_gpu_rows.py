@@ -554,3 +554,22 @@ def test_calls_on_the_graphs_of_a_set_share_its_cache():
             outs.append((q, o, m.k.clone(), m.v.clone()))
         assert all(torch.equal(_bits(u), _bits(w)) for u, w in zip(*outs))
     s.destroy()
+
+
+@pytest.mark.parametrize("kw", [dict(n_q=8, n_kv=2, d=128, qk_norm=True), dict(n_q=16, n_kv=2, d=64, page=16, pages=260), dict(n_q=3, n_kv=3, d=64)])
+@pytest.mark.parametrize("lens", [[20, 0, 7], [300, 1, 211], [3, 500, 430]])
+def test_many_rows_in_place(lens, kw):
+    """Up to and above 512 rows, a wavefront has other groups of heads: the same bits as with the queries in a place of their own."""
+    m = RowsModel(batch=3, max_seq=1024, **kw)
+    pos, slots, begin, width = [500, 3, 17], [1, 2, 0], _begin(lens, 2), m.n_q * m.d
+    x = m.normal(begin[-1] + 3, (m.n_q + 2 * m.n_kv) * m.d + 16)
+    q = x[:, :width].clone()
+    k0, v0, y = m.k.clone(), m.v.clone(), x.clone()
+    m.append(1, begin, slots, pos, x, q)
+    m.status()
+    k1, v1 = m.k.clone(), m.v.clone()
+    m.k.copy_(k0), m.v.copy_(v0)
+    m.append(1, begin, slots, pos, y, y)
+    m.status()
+    assert torch.equal(_bits(y[:, :width]), _bits(q)) and torch.equal(_bits(y[:, width:]), _bits(x[:, width:]))
+    assert torch.equal(_bits(m.k), _bits(k1)) and torch.equal(_bits(m.v), _bits(v1)) and not torch.equal(_bits(k1), _bits(k0))
