@@ -573,3 +573,30 @@ def test_many_rows_in_place(lens, kw):
     m.status()
     assert torch.equal(_bits(y[:, :width]), _bits(q)) and torch.equal(_bits(y[:, width:]), _bits(x[:, width:]))
     assert torch.equal(_bits(m.k), _bits(k1)) and torch.equal(_bits(m.v), _bits(v1)) and not torch.equal(_bits(k1), _bits(k0))
+
+
+# More runs of a tile than a wavefront of the join has lanes (144, 214, 137, and 167 of one row in a call with rows to spare, twice as
+# long as they would be for the runs to be no more than the join holds); more units than run at once, tiles of several sequences (520,
+# 544) and single rows of many heads (768 and 1152, a workgroup takes several).
+MANY = [
+    dict(n_q=1, n_kv=1, d=64, lens=[129], pos=[64000], slots=None, max_seq=64192, batch=1, layers=1),
+    dict(n_q=1, n_kv=1, d=64, lens=[129], pos=[150000], slots=None, max_seq=150200, batch=1, layers=1),
+    dict(n_q=2, n_kv=1, d=128, lens=[129], pos=[96000], slots=None, max_seq=96192, batch=1, layers=1, page=64, pages=1503),
+    dict(n_q=1, n_kv=1, d=64, lens=[1], pos=[64000], slots=None, max_seq=64192, batch=1, layers=1, behind=199),
+    dict(n_q=8, n_kv=8, d=128, lens=[1100, 1, 700, 300, 0, 900, 64, 1300], pos=[5, 3000, 1700, 0, 9, 40, 2900, 2600], slots=[3, 1, 0, 2, 7, 6, 5, 4],
+         max_seq=4000, batch=8, layers=1),
+    dict(n_q=16, n_kv=8, d=64, lens=[600, 1, 350, 150, 0, 450, 32, 650], pos=[5, 3000, 1700, 0, 9, 40, 2900, 2600], slots=None, max_seq=4000,
+         batch=8, layers=1, page=16, pages=2003),
+    dict(n_q=32, n_kv=32, d=128, lens=[1] * 16, pos=[256 * (7 * i % 16 + 1) for i in range(16)], slots=None, max_seq=4200, batch=16, layers=1),
+    dict(n_q=48, n_kv=48, d=64, lens=[1] * 16, pos=[256 * (7 * i % 16 + 1) for i in range(16)], slots=None, max_seq=4200, batch=16, layers=1),
+]
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_attend_many_runs_and_units(case):
+    m, lens, pos, slots, begin, q = _attend_case(case)
+    out = m.normal(q.shape[0], m.n_q * m.d)
+    before = out.clone()
+    m.attend(0, begin, slots, pos, q, out, workspace())
+    m.status()
+    _check_attend(m, 0, lens, pos, slots, begin, q, out, before)
