@@ -600,3 +600,14 @@ def test_attend_many_runs_and_units(case):
     m.attend(0, begin, slots, pos, q, out, workspace())
     m.status()
     _check_attend(m, 0, lens, pos, slots, begin, q, out, before)
+
+
+def test_a_call_of_no_rows_does_nothing():
+    """Not even a workspace or a buffer is needed, and the sequences may say anything but NULL."""
+    m = RowsModel(n_q=8, n_kv=2, d=64)
+    k0, v0, lists = m.k.clone(), m.v.clone(), m.ints([0, 0, 0])
+    m.graph.rows_append(1, 2, 0, lists.data_ptr(), 0, lists.data_ptr(), 0, M.ROWS_F32, 0, 0, 0)
+    m.graph.rows_attend(1, 2, 0, lists.data_ptr(), 0, lists.data_ptr(), 0, 0, 0, 0, 0)
+    m.graph.rows_logprobs(0, 0, M.ROWS_F32, 0, 0, 4, 0, 0, 0, 0, 0)
+    m.status()
+    assert torch.equal(_bits(m.k), _bits(k0)) and torch.equal(_bits(m.v), _bits(v0))

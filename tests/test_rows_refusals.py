@@ -81,6 +81,17 @@ def test_no_rows_need_no_buffers():
     _refused(g.rows_attend, *dict(attend, layer=9).values(), match="layer")
 
 
+def test_no_rows_need_no_buffers_none_of_them():
+    """Every buffer of the rows is NULL, with strides of nothing; one name that a call does not have would be a mistake here."""
+    g = RowsModel(host_only=True).graph
+    for call, args, none in ((g.rows_append, APPEND, ("qkv", "stride", "q", "q_stride")), (g.rows_attend, ATTEND, ("q", "q_stride", "out", "out_stride", "work")),
+                             (g.rows_logprobs, LOGITS, ("logits", "stride", "tokens", "logprobs", "entropy", "top_tokens", "top_logprobs", "work"))):
+        empty = dict(args, n_rows=0, **dict.fromkeys(none, 0))
+        assert list(empty) == list(args)
+        _refused(call, *empty.values(), match="host_only")
+        _refused(call, *dict(empty, n_rows=1).values(), match="NULL")
+
+
 def test_a_cache_too_long_for_the_cuts():
     g = RowsModel(max_seq=(1 << 28) + 8, batch=1, host_only=True).graph
     for call in (lambda: g.rows_append(*APPEND.values()), lambda: g.rows_attend(*ATTEND.values())):
