@@ -611,3 +611,35 @@ def test_a_call_of_no_rows_does_nothing():
     m.graph.rows_logprobs(0, 0, M.ROWS_F32, 0, 0, 4, 0, 0, 0, 0, 0)
     m.status()
     assert torch.equal(_bits(m.k), _bits(k0)) and torch.equal(_bits(m.v), _bits(v0))
+
+
+def test_two_graphs_at_once_cut_their_rows():
+    """Rows of logits in runs, joined through each graph's own counters and each call's own workspace."""
+    rows, vocab, k = 6, 150011, 20
+    sides = []
+    for seed in (1, 2):
+        m = RowsModel(n_q=4, n_kv=2, d=64, batch=1, layers=1, max_seq=64, vocab=vocab, seed=seed)
+        x = m.normal(rows, vocab, dtype=torch.float32)
+        sides.append(SimpleNamespace(m=m, x=x, tokens=m.ints([7 * seed] * rows), work=workspace(), stream=torch.cuda.Stream(), outs=[]))
+
+    def run(s, stream):
+        with torch.cuda.stream(stream):
+            lp, ent = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+            ids, tops = torch.empty(rows, k, dtype=torch.int32, device="cuda"), torch.empty(rows, k, device="cuda")
+            s.m.graph.rows_logprobs(rows, s.x.data_ptr(), M.ROWS_F32, vocab, s.tokens.data_ptr(), k, lp.data_ptr(), ent.data_ptr(), ids.data_ptr(),
+                                    tops.data_ptr(), s.work.data_ptr(), stream.cuda_stream)
+        return lp, ent, ids, tops
+
+    alone = []
+    for s in sides:
+        alone.append(run(s, torch.cuda.current_stream()))
+        s.m.status()
+        best = s.x.double().sort(dim=-1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(alone[-1][2].long(), best)
+    for _ in range(30):
+        for s in sides:
+            s.outs.append(run(s, s.stream))
+    for s, want in zip(sides, alone):
+        s.m.status()
+        for got in s.outs:
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
