@@ -546,7 +546,8 @@ void mpk_serve_destroy(mpk_server *s);
  *
  * Common to the three
  *   - the graph says which model, cache, page table and GPU; it is not host_only, not a serving graph
- *     (its slots and pages belong to its server) and lives on the current device.  Whole models and
+ *     (its slots, pages and error word belong to its server; the logits that a server leaves are scored
+ *     through any other graph of the same vocabulary) and lives on the current device.  Whole models and
  *     one graph of a set work alike (a set's graph sees the first `batch` slots).
  *   - asynchronous on `stream`; no allocation, no host synchronisation; may be captured into a HIP
  *     graph (all lengths are read from device memory when the work runs, so a replay follows them).
@@ -627,7 +628,8 @@ mpk_status mpk_rows_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  *   workspace    : device, MPK_ROWS_WORKSPACE_BYTES
  * A logit of -inf is a token ruled out: ln p = -inf, nothing for the entropy.  A row that holds a NaN or
  * +inf, or nothing above -inf, has no distribution: logprob (of a token asked about), entropy and
- * top_logprobs are NaN, top_tokens -1.  Device error: a token outside -1 .. vocab - 1 (its logprob is NaN). */
+ * top_logprobs are NaN, top_tokens -1.  Device error: a token outside -1 .. vocab - 1 (its logprob is NaN;
+ * mpk_graph_status names its row). */
 #define MPK_ROWS_MAX_TOP 32u
 mpk_status mpk_rows_logprobs(mpk_graph *g, uint32_t n_rows, const void *logits, uint32_t logits_type,
                              size_t row_stride, const int32_t *tokens, float *logprobs, float *entropy,

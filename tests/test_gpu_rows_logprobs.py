@@ -265,3 +265,31 @@ def test_captured_and_on_another_stream():
         assert torch.equal(ids.long(), x.double().sort(dim=-1, descending=True, stable=True).indices[:, :20])
         assert (tops - p.gather(1, ids.long())).abs().max() < 1e-4
     g.status()
+
+
+def test_what_a_server_decodes_is_scored_through_another_graph():
+    """A serving graph refuses the calls on rows; any other graph of the vocabulary takes the logits that its server left."""
+    m = RowsModel(n_q=4, n_kv=2, d=64, batch=2, layers=2, vocab=9001, max_seq=64, page=16, pages=20, fill=0.0)
+    ptrs = {n: t.data_ptr() for n, t in m.outer.items()}
+    ptrs["layers"] = [{n: t.data_ptr() for n, t in w.items()} for w in m.w]
+    served = M.compile_graph(m.shape, ptrs, (m.k.data_ptr(), m.v.data_ptr()), fusion=31, transitive_reduction=1, kv_page_size=16, kv_pages=20,
+                             serving=1, greedy_loop=1)
+    server = served.serve(4, 8, 8)
+    for prompt in ([5, 900, 17], [8000, 1, 2]):
+        server.submit(prompt, 8)
+    server.run(10)   # (three tokens of the prompt; the eighth new one of both sequences is what the last iteration sampled)
+    torch.cuda.synchronize()
+    server.status()
+    last = server.state()["tokens"]
+    lp, en, work = torch.empty(2, device="cuda"), torch.empty(2, device="cuda"), workspace()
+    tops, best = torch.empty(2, 5, device="cuda"), torch.empty(2, 5, dtype=torch.int32, device="cuda")
+    with pytest.raises(M.MpkError, match="server"):
+        served.rows_logprobs(2, server.logits_ptr(), M.ROWS_F32, 9001, 0, 5, 0, en.data_ptr(), best.data_ptr(), tops.data_ptr(), work.data_ptr())
+    tokens = m.ints(last)
+    m.graph.rows_logprobs(2, server.logits_ptr(), M.ROWS_F32, 9001, tokens.data_ptr(), 5, lp.data_ptr(), en.data_ptr(), best.data_ptr(),
+                          tops.data_ptr(), work.data_ptr())
+    m.status()
+    server.status()
+    assert best[:, 0].tolist() == last   # (greedy: what was sampled is the most probable)
+    assert torch.isfinite(lp).all() and torch.equal(lp, tops[:, 0]) and (en > 0).all()
+    server.destroy()
