@@ -606,7 +606,8 @@ mpk_status mpk_rows_append(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  *         16-byte aligned, strides multiples of 8 elements
  *   workspace : device, MPK_ROWS_WORKSPACE_BYTES
  * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to bf16 for the product with
- * V, the output once at the end.  Cache rows above a row's position never reach it, whatever they hold
+ * V, the output once at the end.  A decode step keeps queries, probabilities and outputs in fp32: the same
+ * token through it and through these calls differs by those roundings.  Cache rows above a row's position never reach it, whatever they hold
  * (NaN and infinities included).
  * Device errors as above; with a page outside the pool the sequence's outputs are undefined. */
 mpk_status mpk_rows_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows,

@@ -104,7 +104,8 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
 // angle position inv_freq[i], which is worked out and reduced to one turn in 64 bits.
 // A wavefront takes one row and G groups of its heads; a group is 64 / LPH heads, a head LPH lanes, a lane 8
 // elements of the head's lower half and the 8 they are rotated with.  Bound by memory: 8192 rows of 64 + 2 x 8 heads of 128, 336 MB
-// read and written, 60 us, 5.6 TB/s (a copy of 1 GiB reaches 5.07: part of this fits the last cache).
+// read and written, 60 us, 5.6 TB/s (a copy of 1 GiB reaches 5.07: part of this fits the last cache).  Queries leave in bf16 whatever
+// they come in, as the matrix cores take them.
 template <typename T, int D, uint32_t G>
 __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t waves_per_row) {
   constexpr uint32_t LPH = D / 16, HPG = 64 / LPH, HALF = D / 2;
@@ -209,8 +210,13 @@ hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream)
 // K and V tiles go from memory straight into LDS, the next block's while this one is worked on, their 16-byte pieces permuted
 // (place ^ swizzle(row)) so that neither 16 rows at one place nor 4 rows at 64 bytes share a bank.
 // What bounds it: many rows, the card's power, which takes the clock down to 1.8 GHz (2048 tokens over 14000 cached, 64 heads on 8 of 128,
-// 1.01 TFLOP: 937 us, 1.08 PFLOP/s; a product of 8192^3 reaches 1.15 to 1.20 on such values, 1.71 on zeros).  Few rows, the cache's
-// bytes behind 4.5 us to the first of them and 4 us of the join (8 sequences of up to 4096, 75.7 MB: 19.3 us).
+// 1.01 TFLOP: 868 to 911 us, 1.11 to 1.16 PFLOP/s; a product of 8192^3 reaches 1.15 to 1.20 on such values in a long run, 1.42 in a short
+// one, 1.71 on zeros).  Few rows, the cache's bytes behind 4.5 us to the first of them and 4 us of the join (8 sequences of up to 4096,
+// 75.7 MB: 17.5 to 19.2 us on a cache that the last call left behind, 21 to 23 over ten layers' in turn).
+// Rounded: the queries, which come in bf16, and the probabilities; all else is fp32.  In one term of bf16 a probability costs the output 0.0016
+// of its size beside the 0.0016 of its own rounding (0.0018 to 0.0024 together, against 64 bits).  In two terms, V P_hi + V P_lo, 0.0016 in
+// all, and half as many products again: one / two terms, 4096 tokens 136 / 192 us, 2048 over 14000 907 / 1311, 16 ragged prompts 147 / 200,
+// 8 x 1 token 19.2 / 19.9, 5 over 30000 18.1 / 19.8.  (A decode step, which waits for memory, has three and fp32 queries.)
 constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
@@ -737,7 +743,9 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   const uint32_t grid = (uint32_t)std::min<uint64_t>(tiles <= kAttendSlots / 2u ? kAttendSlots : tiles + (tiles <= 2u * kAttendSlots ? kAttendSlots : kAttendSlots / 4u), 1u << 20);
   // Rows of one tile at most: keys that are kept would only drive out others from the caches.  (Kept / not, 10 layers' caches in turn: 8 x 1
   // token over 512 to 4096 24.7 / 22.8 us, 16 x 1 over 4000 52.6 / 47.9; one call's cache, which stays in the last cache, 21.9 / 21.9.  Several
-  // tiles a sequence, 16 ragged prompts: 147 / 159.)
+  // tiles a sequence, 16 ragged prompts: 147 / 159.)  By the rows of the call, for the host does not see the sequences': more rows than a tile
+  // has, of sequences that have one tile each, go the other way, as do few rows in a call with many to spare (8 x 4 / 8 x 5 tokens over 4000,
+  // 26.0 / 27.8 us; 16 x 2 / 16 x 3 over 2000, heads of 64, 15.3 / 19.0).
   if (a.s.n_rows << lg <= kTileRows) {
     const uint32_t runs = std::min(kAttendFewChunks, a.s.max_seq / (kAttendMinBlocks * kBlockKeys) + 1u);
     rows_attend_kernel<D, PAGED, true><<<dim3(std::min(attend_slots(D, true), a.s.n_seqs * a.s.n_kv * runs)), dim3(256), attend_lds(D), stream>>>(a, lg);
@@ -745,6 +753,8 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   else rows_attend_kernel<D, PAGED, false><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
+  // On a longer cache the host cannot tell whether anything was cut, so a call that was not pays for the launch (64 tokens, max_seq 64 / 4096:
+  // 7.5 / 10.1 us).
   const uint64_t items = (uint64_t)a.s.n_rows * a.s.n_q;
   if (items <= kJoinFewItems) rows_attend_join_kernel<D, 4><<<dim3((uint32_t)items), dim3(256), 0, stream>>>(a, lg);
   else rows_attend_join_kernel<D, 1><<<dim3((uint32_t)std::min<uint64_t>((items + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
@@ -764,9 +774,11 @@ hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
 // best logits, sorted, one a lane.  A step none of whose logits beats the last of these, most of them, is sums alone.
 // With few rows a row is cut into runs of steps, one a workgroup, and the one that arrives last joins these.
 // What bounds it: many rows, the vector operations (an unpack, a half of a maximum, a fused product, an exponential at a quarter of
-// the rate, a floor and two sums a logit: 4096 rows of 32000 bf16, 262 MB, 53 to 58 us with 4 alternatives, 50 with none); in fp32 memory
-// (4096 rows with 5 83 us, 6.3 TB/s).  One row of 151936 with 20, 11 us: what waits for what, a fifth of it each the first logits, the
-// first step's alternatives, a run's join, its way to the others and the row's join.
+// the rate, a floor, a fused product and a sum a logit, and what a load takes: 118 for the 16 logits of a lane's step.  Of the 5500 of a
+// row of 32000 that is two thirds; the others are the steps, ten or so of 32 with 4 alternatives, that have one to offer or a new maximum.
+// 4096 rows of 32000 bf16, 262 MB, 53 to 58 us with 4 alternatives, 50 with none); in fp32 memory (4096 rows with 5 83 us, 6.3 TB/s).
+// One row of 151936 with 20, 11 us: what waits for what, a fifth of it each the first logits, the first step's alternatives, a run's
+// join, its way to the others and the row's join.
 constexpr uint32_t kLogprobChunks = 64;   // runs of a row at most: a lane each when they are joined
 // Workgroups that a call is cut into where its rows are fewer.  512 / 1024 / 1536 with 20 alternatives: 32 rows of 151936 19.2 / 18.2 /
 // 16.9 us, 64 23.2 / 23.7 / 23.2, 200 37.0 / 35.8 / 40.1; 200 of 32000 20.2 / 18.9 / 20.6, 512 23.7 / 25.8 / 32.0.
