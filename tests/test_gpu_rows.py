@@ -643,3 +643,25 @@ def test_two_graphs_at_once_cut_their_rows():
         s.m.status()
         for got in s.outs:
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("case", [ATTEND[i] for i in (3, 5, 6, 9, 10)])
+def test_a_query_that_is_not_finite_reaches_its_own_row_and_head_alone(case, bad):
+    m, lens, pos, slots, begin, q = _attend_case(case)
+    out, poisoned = torch.empty_like(q), torch.empty_like(q)
+    m.attend(m.layers - 1, begin, slots, pos, q, out, workspace())
+    m.status()
+    hit = torch.zeros(q.shape[0], m.n_q, dtype=torch.bool, device=m.dev)
+    for i, n in enumerate(lens):
+        for t in range(0, n, 7):
+            hit[begin[i] + t, (3 * t + i) % m.n_q] = True
+    q.view(-1, m.n_q, m.d)[..., 5].masked_fill_(hit, bad)
+    m.attend(m.layers - 1, begin, slots, pos, q, poisoned, workspace())
+    m.status()
+    a, b = out.view(-1, m.n_q, m.d), poisoned.view(-1, m.n_q, m.d)
+    for i, n in enumerate(lens):
+        r = slice(begin[i], begin[i] + n)
+        clean = ~hit[r]
+        assert torch.equal(_bits(a[r][clean]), _bits(b[r][clean]))
+        assert b[r][hit[r]].isnan().all()   # (infinite scores have no softmax)
