@@ -637,6 +637,95 @@ mpk_status mpk_rows_logprobs(mpk_graph *g, uint32_t n_rows, const void *logits, 
                              uint32_t n_top, int32_t *top_tokens, float *top_logprobs, void *workspace,
                              void *stream);
 
+/* ----------------------------------------------------------------------------------------------
+ * Trees of drafted tokens on the cache of a compiled graph: a program that guesses several tokens ahead has
+ * them all looked at in one pass over the weights, keeps what the model agrees with and decodes on.  It runs the
+ * projections itself, as with rows of prompts: mpk_tree_append and mpk_tree_attend once a layer, mpk_tree_verify on the
+ * logits of the nodes, mpk_tree_keep once, for all layers.  Everything that the next step needs stays in device memory.
+ *
+ * A tree is a sequence's rows of the call, at most MPK_TREE_MAX_NODES (sequences of no rows are allowed, and are left
+ * alone).  The row at place t of its sequence, counted from 0, is node t; parents[row] is the place of its parent, below t, or -1.
+ * With `positions[i]` rows of the sequence cached, node t is cached at row positions[i] + t, stands at position
+ * positions[i] + depth(t), depth being the number of its ancestors, and sees the rows cached before, its
+ * ancestors and itself.  A chain is what mpk_rows_append and mpk_rows_attend would make of the same rows.
+ *
+ * Common to the four: what is common to the calls on rows above, their workspace and errors included.  The cache rows behind the
+ * accepted ones hold rejected nodes afterwards; nothing reads them before they are written again.
+ * -------------------------------------------------------------------------------------------- */
+#define MPK_TREE_MAX_NODES 256u
+
+/* mpk_rows_append for nodes: their angles go by positions[i] + depth, their cache rows by positions[i] + place.
+ *   parents : device int32 [n_rows]
+ *   others  : as mpk_rows_append
+ * Device errors as mpk_rows_append; also more nodes than MPK_TREE_MAX_NODES, a parent that is no earlier node (the sequence is
+ * left out). */
+mpk_status mpk_tree_append(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows,
+                           const int32_t *row_begin, const int32_t *slots, const int32_t *positions,
+                           const int32_t *parents, const void *qkv, uint32_t qkv_type, size_t qkv_stride,
+                           void *q_out, size_t q_stride, void *stream);
+
+/* mpk_rows_attend for nodes: node t attends to cache rows 0 .. positions[i] - 1, to its ancestors' and its own.  What the cache
+ * holds in other nodes' rows never reaches it (NaN and infinities included).
+ *   parents : device int32 [n_rows]
+ *   others  : as mpk_rows_attend
+ * Device errors as mpk_rows_attend; also more nodes than MPK_TREE_MAX_NODES (the sequence is left out), a parent that is
+ * no earlier node (the sequence's outputs are undefined). */
+mpk_status mpk_tree_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows,
+                           const int32_t *row_begin, const int32_t *slots, const int32_t *positions,
+                           const int32_t *parents, const void *q, size_t q_stride, void *out, size_t out_stride,
+                           void *workspace, void *stream);
+
+/* Which drafted tokens stay, and the token behind them.  A tree has one root here: node 0, the token decoded last (parent -1, no
+ * other node has); its children are guesses at the next token, theirs at the one after.  The walk starts at the root with
+ * r = p = softmax(row of the node / temperature) and takes the node's children in order of their rows; child c with token x is
+ * accepted if
+ *     uniforms[c] q(x) < r(x),
+ * else r becomes max(0, r - q) / its sum (r as it is where nothing would be left).  The walk goes on at an accepted child;
+ * if there is none, the next token is drawn from r: the first v with sum_{w <= v} r(w) > uniforms[root].  q is what x was drawn from:
+ *   draft_probs NULL : x was chosen, not drawn: q is 1 at x, so that c is accepted with the probability r(x)
+ *   draft_probs      : row of the node, the children were drawn from it independently
+ *   ... and MPK_TREE_DRAWN_ONCE : without replacement: q times 1 / (1 - sum of q over the earlier children's tokens);
+ *                      a child is never accepted where that sum has reached 1
+ * With uniform random numbers that nothing else has used, the tokens then have the distribution of tokens drawn one by one from p.
+ * temperature 0: greedy: the child with the largest logit's token, of equal logits the lower index, is accepted, and the largest
+ * is the next token.
+ *   n_seqs, n_rows, row_begin : as above (the graph's cache and positions are not looked at)
+ *   parents, tokens : device int32 [n_rows].  A root's token is not looked at
+ *   logits       : device [n_rows][row stride row_stride elements], bf16 or fp32 (logits_type), over the graph's vocab.  Any
+ *                  alignment of the element type, any stride >= vocab
+ *   draft_probs  : device fp32 [n_rows][row stride draft_stride >= vocab], none negative, or NULL.  Only rows of nodes with children are read
+ *   flags        : MPK_TREE_DRAWN_ONCE or 0
+ *   temperatures : device fp32 [n_seqs], finite, not negative; NULL: 0 for all
+ *   uniforms     : device fp32 [n_rows], 0 <= u < 1: of a child for its acceptance, of a root for the next token.  Not looked
+ *                  at for temperature 0, NULL only with temperatures
+ *   lengths      : device int32 [n_seqs]: nodes on the accepted path, the root included; 0 for a sequence without rows or left out
+ *   path         : device int32 [n_rows]: their places, ascending, in the sequence's first lengths[i] rows; -1 in its others
+ *   next_tokens  : device int32 [n_seqs]: the token behind the path; -1: none
+ *   logprobs     : device fp32 [n_rows] or NULL: in the place of a path's node, ln p of the token behind that node (the path's next, or
+ *                  next_tokens); 0 in the sequence's others.  (temperature 0: p is of the logits as they are)
+ *   workspace    : device, MPK_ROWS_WORKSPACE_BYTES
+ * p, r, sums and comparisons are in 64 bits.  A logit of -inf is a token ruled out.  At a node whose row holds a NaN or +inf, or nothing
+ * above -inf, the walk ends: next_tokens is -1, its logprob NaN.
+ * Device errors: row_begin not ascending or outside 0 .. n_rows (lengths 0, next_tokens -1, nothing else is written); more nodes than
+ * MPK_TREE_MAX_NODES, a parent that is no earlier node, a temperature that is negative or not finite (the sequence is
+ * left out: its path is -1, its logprobs 0); a token outside 0 .. vocab - 1 that the walk comes to (never accepted). */
+#define MPK_TREE_DRAWN_ONCE 1u
+mpk_status mpk_tree_verify(mpk_graph *g, uint32_t n_seqs, uint32_t n_rows, const int32_t *row_begin,
+                           const int32_t *parents, const int32_t *tokens, const void *logits, uint32_t logits_type,
+                           size_t row_stride, const float *draft_probs, size_t draft_stride, uint32_t flags,
+                           const float *temperatures, const float *uniforms, int32_t *lengths, int32_t *path,
+                           int32_t *next_tokens, float *logprobs, void *workspace, void *stream);
+
+/* The cache rows of an accepted path close up, K and V of every layer: row positions[i] + path[row_begin[i] + k] moves to
+ * positions[i] + k, for k below lengths[i].  (A node of the path at place k of it has depth k: its row has the angle of where it then is.)
+ *   n_seqs .. positions : as above;  lengths, path : as mpk_tree_verify leaves them
+ *   positions_out : device int32 [n_seqs] or NULL: positions[i] + lengths[i], what the next step starts from; not `positions`
+ * Device errors as mpk_tree_append; also a length outside 0 .. the tree's nodes, a path that does not ascend within
+ * it (the sequence is left out, its position stays), a page outside the pool (its rows are left out). */
+mpk_status mpk_tree_keep(mpk_graph *g, uint32_t n_seqs, uint32_t n_rows, const int32_t *row_begin,
+                         const int32_t *slots, const int32_t *positions, const int32_t *lengths,
+                         const int32_t *path, int32_t *positions_out, void *stream);
+
 const char *mpk_last_error(void);
 void mpk_graph_destroy(mpk_graph *g);
 

@@ -107,9 +107,11 @@ SYMBOLS = ("mpk_compile", "mpk_compile_dag", "mpk_decode_step", "mpk_decode_step
            "mpk_graph_set_page_table", "mpk_serve_create", "mpk_serve_submit", "mpk_serve_run",
            "mpk_serve_result", "mpk_serve_state", "mpk_serve_logits", "mpk_serve_destroy",
            "mpk_serve_create_set", "mpk_serve_last_batch", "mpk_serve_status", "mpk_graph_task_forms",
-           "mpk_rows_append", "mpk_rows_attend", "mpk_rows_logprobs")
+           "mpk_rows_append", "mpk_rows_attend", "mpk_rows_logprobs", "mpk_tree_append", "mpk_tree_attend", "mpk_tree_verify",
+           "mpk_tree_keep")
 ROWS_BF16, ROWS_F32 = 0, 1
 ROWS_MAX_TOP, ROWS_WORKSPACE_BYTES = 32, 96 << 20
+TREE_MAX_NODES, TREE_DRAWN_ONCE = 256, 1
 DEBUG_TRACE, DEBUG_POISON, DEBUG_JITTER, DEBUG_LOSE_NOTIFY = 1, 2, 4, 8
 
 _lib = None
@@ -176,7 +178,12 @@ def lib():
         L.mpk_rows_append.argtypes = seqs + [vp, C.c_uint32, C.c_size_t, vp, C.c_size_t, vp]
         L.mpk_rows_attend.argtypes = seqs + [vp, C.c_size_t, vp, C.c_size_t, vp, vp]
         L.mpk_rows_logprobs.argtypes = [vp, C.c_uint32, vp, C.c_uint32, C.c_size_t, vp, vp, vp, C.c_uint32, vp, vp, vp, vp]
+        L.mpk_tree_append.argtypes = seqs + [vp, vp, C.c_uint32, C.c_size_t, vp, C.c_size_t, vp]
+        L.mpk_tree_attend.argtypes = seqs + [vp, vp, C.c_size_t, vp, C.c_size_t, vp, vp]
+        L.mpk_tree_verify.argtypes = [vp, C.c_uint32, C.c_uint32, vp, vp, vp, vp, C.c_uint32, C.c_size_t, vp, C.c_size_t, C.c_uint32] + [vp] * 8
+        L.mpk_tree_keep.argtypes = [vp, C.c_uint32, C.c_uint32] + [vp] * 7
         for n in SYMBOLS[:14] + ("mpk_rows_append", "mpk_rows_attend", "mpk_rows_logprobs",
+                                 "mpk_tree_append", "mpk_tree_attend", "mpk_tree_verify", "mpk_tree_keep",
                                  "mpk_graph_set_page_table", "mpk_serve_create", "mpk_serve_submit", "mpk_serve_run", "mpk_serve_result", "mpk_serve_state"):
             getattr(L, n).restype = C.c_int
         _lib = L
@@ -291,6 +298,34 @@ class Graph:
         _check(lib().mpk_rows_logprobs(self._h, n_rows, logits_ptr, logits_type, row_stride, tokens_ptr or None, logprobs_ptr or None,
                                        entropy_ptr or None, n_top, top_tokens_ptr or None, top_logprobs_ptr or None, workspace_ptr,
                                        stream))
+
+    def tree_append(self, layer: int, n_seqs: int, n_rows: int, row_begin_ptr: int, slots_ptr: int, positions_ptr: int, parents_ptr: int,
+                    qkv_ptr: int, qkv_type: int, qkv_stride: int, q_out_ptr: int, q_stride: int, stream: int = 0):
+        """rows_append for the nodes of trees: rotated by their depth, appended in their order."""
+        _check(lib().mpk_tree_append(self._h, layer, n_seqs, n_rows, row_begin_ptr, slots_ptr or None, positions_ptr, parents_ptr, qkv_ptr,
+                                     qkv_type, qkv_stride, q_out_ptr, q_stride, stream))
+
+    def tree_attend(self, layer: int, n_seqs: int, n_rows: int, row_begin_ptr: int, slots_ptr: int, positions_ptr: int, parents_ptr: int,
+                    q_ptr: int, q_stride: int, out_ptr: int, out_stride: int, workspace_ptr: int, stream: int = 0):
+        """rows_attend for the nodes of trees: each sees the rows cached before, its ancestors and itself."""
+        _check(lib().mpk_tree_attend(self._h, layer, n_seqs, n_rows, row_begin_ptr, slots_ptr or None, positions_ptr, parents_ptr, q_ptr,
+                                     q_stride, out_ptr, out_stride, workspace_ptr, stream))
+
+    def tree_verify(self, n_seqs: int, n_rows: int, row_begin_ptr: int, parents_ptr: int, tokens_ptr: int, logits_ptr: int,
+                    logits_type: int, row_stride: int, draft_probs_ptr: int, draft_stride: int, flags: int, temperatures_ptr: int,
+                    uniforms_ptr: int, lengths_ptr: int, path_ptr: int, next_tokens_ptr: int, logprobs_ptr: int, workspace_ptr: int,
+                    stream: int = 0):
+        """Which drafted tokens the logits and the random numbers accept, and the token behind them; what is not given or not
+        wanted is 0 (no draft_probs: tokens that were chosen; no temperatures: greedy)."""
+        _check(lib().mpk_tree_verify(self._h, n_seqs, n_rows, row_begin_ptr, parents_ptr, tokens_ptr, logits_ptr, logits_type, row_stride,
+                                     draft_probs_ptr or None, draft_stride, flags, temperatures_ptr or None, uniforms_ptr or None,
+                                     lengths_ptr, path_ptr, next_tokens_ptr, logprobs_ptr or None, workspace_ptr, stream))
+
+    def tree_keep(self, n_seqs: int, n_rows: int, row_begin_ptr: int, slots_ptr: int, positions_ptr: int, lengths_ptr: int, path_ptr: int,
+                  positions_out_ptr: int, stream: int = 0):
+        """The accepted paths' rows close up behind the cached ones, in every layer; positions_out_ptr 0: not wanted."""
+        _check(lib().mpk_tree_keep(self._h, n_seqs, n_rows, row_begin_ptr, slots_ptr or None, positions_ptr, lengths_ptr, path_ptr,
+                                   positions_out_ptr or None, stream))
 
     def serve(self, max_requests: int, max_prompt: int, max_new: int, eos_token: int = -1) -> "Server":
         cfg = ServeConfig(C.sizeof(ServeConfig), max_requests, max_prompt, max_new, eos_token)

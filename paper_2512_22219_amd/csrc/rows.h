@@ -1,4 +1,5 @@
-// Rows beside the decode step (mpk_rows_*): what the host side hands to the kernels of rows.hip.
+// Rows beside the decode step (mpk_rows_*) and trees of drafted tokens (mpk_tree_*): what the host side hands to the kernels of
+// rows.hip and tree.hip.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -7,6 +8,7 @@
 namespace mpk {
 
 constexpr uint32_t kMaxRowSeqs = 16;   // sequences of a call: at most a graph's batch
+constexpr uint32_t kTreeNodes = MPK_TREE_MAX_NODES;   // nodes of a tree
 // A graph's counters of the workgroups that have finished their part of a row, zero between calls; each on a line of its own (16
 // rows of 32 parts: 11.0 us, counted on one line 15.4).
 constexpr uint32_t kRowsArrivals = 1024, kArrivalStride = 32;
@@ -33,6 +35,7 @@ struct AppendArgs {
   const uint16_t *q_norm, *k_norm;   // null: no norm
   const double* inv_freq;
   float eps;
+  const int32_t* parents;   // [n_rows]: the rows are nodes of trees; else null
 };
 
 struct AttendArgs {
@@ -41,6 +44,7 @@ struct AttendArgs {
   uint16_t* out;
   size_t q_stride, out_stride;   // elements
   void* work;
+  const int32_t* parents;   // as above
 };
 
 struct LogprobArgs {
@@ -55,11 +59,36 @@ struct LogprobArgs {
   uint32_t *err, *arrivals;
 };
 
+struct VerifyArgs {
+  const int32_t* row_begin;   // [n_seqs + 1]
+  const int32_t *parents, *tokens;   // [n_rows]
+  uint32_t n_seqs, n_rows, vocab, flags;
+  const void* logits;
+  const float* draft;            // null: the tokens were chosen, not drawn
+  size_t stride, draft_stride;   // elements
+  const float *temperatures, *uniforms;   // null: greedy
+  int32_t *lengths, *path, *next;
+  float* logprobs;   // or null
+  void* work;
+  uint32_t* err;
+};
+
+struct KeepArgs {
+  RowSeqs s;   // (k, v: of layer 0)
+  uint32_t n_layers;
+  size_t layer_stride;   // elements of a layer's K or V
+  const int32_t *lengths, *path;
+  int32_t* positions_out;   // or null
+};
+
 // Before any of the others, with the device current: what the kernels need beyond the defaults, once per device.
 hipError_t rows_prepare(int device);
 // Each checks nothing (the entry points have) and launches on `stream`.
-hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream);
+hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream);   // (trees where a.parents is given, here and next)
 hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream);
 hipError_t launch_rows_logprobs(const LogprobArgs& a, bool f32, hipStream_t stream);
+
+hipError_t launch_tree_verify(const VerifyArgs& a, bool f32, hipStream_t stream);
+hipError_t launch_tree_keep(const KeepArgs& a, hipStream_t stream);
 
 }  // namespace mpk

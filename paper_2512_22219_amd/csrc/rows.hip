@@ -1,80 +1,14 @@
-// Rows beside the decode step (mpk_rows_append, mpk_rows_attend, mpk_rows_logprobs): kernels and launches.
+// Rows beside the decode step (mpk_rows_append, mpk_rows_attend, mpk_rows_logprobs), and rows that are the nodes of trees
+// (mpk_tree_append, mpk_tree_attend): kernels and launches.
 #include "rows.h"
 
 #include <algorithm>
 #include <mutex>
 #include <vector>
 
-#include "kernels.h"
+#include "rows_device.h"
 
 namespace mpk {
-
-__device__ __forceinline__ void report_rows(uint32_t* err, uint32_t code, uint32_t d0, uint32_t d1) {
-  if (atomicCAS(&err[0], 0u, code) == 0u) {
-    err[2] = d0;
-    err[3] = d1;
-  }
-}
-
-// The sequences of a call, checked: lane i of the wavefront holds sequence i.  A sequence that is left out has no rows
-// (begin == end).  Every wavefront of every workgroup does this for itself: the loads are one round trip.
-struct SeqLanes {
-  int32_t begin, end, slot, pos;
-};
-__device__ __forceinline__ SeqLanes load_seqs(const RowSeqs& s, bool tell) {
-  const int lane = threadIdx.x & 63;
-  SeqLanes q = {0, 0, -1, 0};
-  if ((uint32_t)lane < s.n_seqs) {
-    q.begin = as_global(s.row_begin)[lane];
-    q.end = as_global(s.row_begin)[lane + 1];
-    q.slot = s.slots ? as_global(s.slots)[lane] : lane;
-    q.pos = as_global(s.positions)[lane];
-  }
-  const uint64_t bad = __ballot(q.begin < 0 || q.end < q.begin || (uint32_t)q.end > s.n_rows);
-  if (bad) {   // no row of the call belongs to anybody for sure
-    const int at = __builtin_ctzll(bad);
-    if (tell && lane == at) report_rows(s.err, DE_BAD_ROWS, (uint32_t)lane, (uint32_t)q.end);
-    return SeqLanes{0, 0, -1, 0};
-  }
-  const int32_t n = q.end - q.begin;
-  uint32_t wrong = DE_NONE, what = 0;
-  if (n > 0) {
-    if (q.slot < 0 || (uint32_t)q.slot >= s.batch) { wrong = DE_BAD_SLOT; what = (uint32_t)q.slot; }
-    else if (q.pos < 0 || (uint32_t)q.pos >= s.max_seq || (uint32_t)n > s.max_seq - (uint32_t)q.pos) {
-      wrong = DE_BAD_POSITION;
-      what = q.pos < 0 || (uint32_t)q.pos >= s.max_seq ? (uint32_t)q.pos : s.max_seq;
-    }
-  }
-  for (uint32_t i = 0; s.slots && i + 1 < s.n_seqs; ++i) {   // (a slot that an earlier sequence with rows has)
-    const int32_t other = __builtin_amdgcn_readlane(q.slot, i), rows = __builtin_amdgcn_readlane(n, i);
-    if (rows > 0 && n > 0 && (uint32_t)lane > i && q.slot == other && !wrong) { wrong = DE_BAD_SLOT; what = (uint32_t)q.slot; }
-  }
-  if (wrong) {
-    if (tell) report_rows(s.err, wrong, (uint32_t)lane, what);
-    q.end = q.begin;
-  }
-  return q;
-}
-
-__device__ __forceinline__ float uniform_f32(float v) { return __uint_as_float(uniform_u32(__float_as_uint(v))); }
-
-// The sequence that row r belongs to (the last that begins at or before it and has it), 64: none.
-__device__ __forceinline__ uint32_t seq_of_row(const SeqLanes& q, uint32_t r) {
-  const uint64_t m = __ballot((uint32_t)q.begin <= r && r < (uint32_t)q.end);
-  return m ? (uint32_t)__builtin_ctzll(m) : 64u;
-}
-
-// Element offset of cache row `row` of (slot, kv head); false: its page is outside the pool.
-__device__ __forceinline__ bool cache_row(const RowSeqs& s, uint32_t slot, uint32_t kvh, uint32_t row, size_t* at) {
-  if (!s.table) {
-    *at = (((size_t)slot * s.n_kv + kvh) * s.max_seq + row) * s.head_dim;
-    return true;
-  }
-  const int32_t page = as_global(s.table)[(size_t)slot * s.blocks + (row >> s.page_shift)];
-  if (page < 0 || (uint32_t)page >= s.n_pages) return false;
-  *at = ((((size_t)page * s.n_kv + kvh) << s.page_shift) + (row & ((1u << s.page_shift) - 1u))) * s.head_dim;
-  return true;
-}
 
 // ------------------------------------------------------------------------------------ append
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -106,19 +40,28 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
 // elements of the head's lower half and the 8 they are rotated with.  Bound by memory: 8192 rows of 64 + 2 x 8 heads of 128, 336 MB
 // read and written, 60 us, 5.6 TB/s (a copy of 1 GiB reaches 5.07: part of this fits the last cache).  Queries leave in bf16 whatever
 // they come in, as the matrix cores take them.
-template <typename T, int D, uint32_t G>
+// TREE: the rows are nodes of trees; a node's angle goes by its depth, its cache row by its place.
+template <typename T, int D, uint32_t G, bool TREE>
 __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t waves_per_row) {
   constexpr uint32_t LPH = D / 16, HPG = 64 / LPH, HALF = D / 2;
   __shared__ float2 angles[4][HALF];
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
-  const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
+  const SeqLanes q = load_seqs<TREE>(s, blockIdx.x == 0 && wave == 0);
   const uint32_t unit = blockIdx.x * 4u + wave, row = unit / waves_per_row, part = unit - row * waves_per_row;
   if (row >= s.n_rows) return;
   const uint32_t seq = seq_of_row(q, row);
   if (seq == 64u) return;
   const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane(q.pos, seq) + row - (uint32_t)__builtin_amdgcn_readlane(q.begin, seq);
   const uint32_t slot = (uint32_t)__builtin_amdgcn_readlane(q.slot, seq);
+  TreeLanes tree;
+  uint32_t wrong = 0, nodes = 0, node = 0;
+  if constexpr (TREE) {   // (on their way beside the rows)
+    const uint32_t begin = (uint32_t)__builtin_amdgcn_readlane(q.begin, seq);
+    nodes = (uint32_t)__builtin_amdgcn_readlane(q.end, seq) - begin;
+    node = row - begin;
+    wrong = load_tree(a.parents + begin, nodes, &tree);
+  }
   const uint32_t sub = lane & (LPH - 1u), heads = s.n_q + 2u * s.n_kv, e = 8u * sub;
   const T* x = (const T*)a.qkv + (size_t)row * a.qkv_stride;
   float lo[G][8], hi[G][8];   // (on their way while the angles are worked out)
@@ -128,9 +71,17 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
     load8(x + (size_t)h * D + e, lo[g]);
     load8(x + (size_t)h * D + HALF + e, hi[g]);
   }
+  uint32_t turn = pos;
+  if constexpr (TREE) {
+    if (wrong < nodes) {
+      if (node == 0 && part == 0 && lane == 0) report_rows(s.err, DE_BAD_PARENT, seq, wrong);
+      return;
+    }
+    turn = pos - node + depth_of(tree, node);
+  }
   if (lane < HALF) {
     const double two_pi = 6.283185307179586476925286766559;
-    double ang = (double)(int32_t)pos * as_global(a.inv_freq)[lane];
+    double ang = (double)(int32_t)turn * as_global(a.inv_freq)[lane];
     ang -= two_pi * rint(ang / two_pi);
     double sn, cs;
     sincos(ang, &sn, &cs);
@@ -182,7 +133,7 @@ __global__ void __launch_bounds__(256) rows_append_kernel(AppendArgs a, uint32_t
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 static hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
   const uint32_t groups = (a.s.n_q + 2u * a.s.n_kv + 1024u / D - 1u) / (1024u / D);
   // A wavefront more a row works out the row's angles once more; a group more a wavefront has fewer of them.  One / two / four groups a
@@ -190,13 +141,17 @@ static hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
   // 4096 19.7 / 18.4 / 19.9.
   const uint32_t per_wave = a.s.n_rows <= 512u ? 1u : 2u, waves_per_row = (groups + per_wave - 1u) / per_wave;
   const dim3 blocks((uint32_t)(((uint64_t)a.s.n_rows * waves_per_row + 3u) / 4u));
-  if (per_wave == 1u) rows_append_kernel<T, D, 1><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
-  else rows_append_kernel<T, D, 2><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
+  if (per_wave == 1u) rows_append_kernel<T, D, 1, TREE><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
+  else rows_append_kernel<T, D, 2, TREE><<<blocks, dim3(256), 0, stream>>>(a, waves_per_row);
   return hipGetLastError();
 }
+template <bool TREE>
+static hipError_t launch_append(const AppendArgs& a, bool f32, hipStream_t stream) {
+  if (a.s.head_dim == 128u) return f32 ? launch_append<float, 128, TREE>(a, stream) : launch_append<uint16_t, 128, TREE>(a, stream);
+  return f32 ? launch_append<float, 64, TREE>(a, stream) : launch_append<uint16_t, 64, TREE>(a, stream);
+}
 hipError_t launch_rows_append(const AppendArgs& a, bool f32, hipStream_t stream) {
-  if (a.s.head_dim == 128u) return f32 ? launch_append<float, 128>(a, stream) : launch_append<uint16_t, 128>(a, stream);
-  return f32 ? launch_append<float, 64>(a, stream) : launch_append<uint16_t, 64>(a, stream);
+  return a.parents ? launch_append<true>(a, f32, stream) : launch_append<false>(a, f32, stream);
 }
 
 // ------------------------------------------------------------------------------------ attend
@@ -366,17 +321,60 @@ __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(
 
 __device__ __forceinline__ uint32_t nonfinite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }   // bit 15 / 31: lower / upper
 
-// ONCE: no sequence has more than one tile, so that a unit's keys are its own.
-template <int D, bool PAGED, bool ONCE>
-__global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) {
+// Which nodes of a tree each node sees, as bits in LDS (256 bits a node): itself and its ancestors.  A thread has a node; in each round it
+// takes over what the farthest ancestor that it has reached has seen, so rounds double the distance.  All 256 threads call this.
+__device__ __forceinline__ void tree_bits(const int32_t* parents, uint32_t nodes, uint32_t seq, uint32_t* err, uint64_t* bits, int16_t* reach) {
+  constexpr uint32_t W = kTreeNodes / 64u;
+  const uint32_t t = threadIdx.x;
+  int32_t p = t < nodes ? as_global(parents)[t] : -1;
+  if (p < -1 || p >= (int32_t)t) {   // (no node sees a later one: the sequence's outputs are wrong, but nothing is read out of place)
+    report_rows(err, DE_BAD_PARENT, seq, t);
+    p = -1;
+  }
+  uint64_t mine[W];
+#pragma unroll
+  for (uint32_t i = 0; i < W; ++i) mine[i] = i == t >> 6 ? 1ull << (t & 63u) : 0ull;
+  for (uint32_t far = 1;; far *= 2u) {
+#pragma unroll
+    for (uint32_t i = 0; i < W; ++i) bits[W * t + i] = mine[i];
+    reach[t] = (int16_t)p;
+    __syncthreads();
+    if (far >= nodes) break;
+    if (p >= 0) {
+#pragma unroll
+      for (uint32_t i = 0; i < W; ++i) mine[i] |= bits[W * p + i];
+      p = reach[p];
+    }
+    __syncthreads();
+  }
+}
+// 64 of a node's bits from the o-th on; those in front of the first are ones (rows cached before the tree).
+__device__ __forceinline__ uint64_t bits_from(const uint64_t* bits, int32_t o) {
+  constexpr int32_t W = kTreeNodes / 64;
+  if (o <= -64) return ~0ull;
+  if (o < 0) return bits[0] << -o | ((1ull << -o) - 1ull);
+  const int32_t i = o >> 6, sh = o & 63;
+  const uint64_t lo = i < W ? bits[i] >> sh : 0ull, hi = sh && i + 1 < W ? bits[i + 1] << (64 - sh) : 0ull;
+  return lo | hi;
+}
+
+constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
+constexpr uint32_t tree_attend_lds(uint32_t D) { return attend_lds(D) + kTreeNodes * (kTreeNodes / 8u + 2u); }
+
+// ONCE: no sequence has more than one tile, so that a unit's keys are its own.  TREE: a row sees the cached rows, its ancestors in the
+// call's tree and itself, where another sees all in front of it and itself.
+template <int D, bool PAGED, bool ONCE, bool TREE>
+__device__ __forceinline__ void attend_units(const AttendArgs& a, uint32_t lg) {
   constexpr uint32_t KS = D / 16, NT = D / 32, CPR = D / 8, RPI = 64 / CPR, IPW = 16 / RPI, ROWB = D * 2, TILE = kBlockKeys * ROWB;
   extern __shared__ __align__(16) unsigned char tiles_lds[];   // K, V of the even blocks, K, V of the odd ones, a flag
   uint32_t& flag = *(uint32_t*)(tiles_lds + 4u * TILE);
+  uint64_t* const bits = (uint64_t*)(tiles_lds + attend_lds(D));   // (trees)
+  int16_t* const reach = (int16_t*)(bits + kTreeNodes * kTreeNodes / 64u);
   const RowSeqs& s = a.s;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), l31 = lane & 31u, half = lane >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
   __builtin_amdgcn_s_setprio(3);   // (until the unit's first requests are out: 8 x 1 token 20.3 / 19.6 us)
-  const SeqLanes q = load_seqs(s, blockIdx.x == 0 && wave == 0);
+  const SeqLanes q = load_seqs<TREE>(s, blockIdx.x == 0 && wave == 0);
   const Deal d = deal_units<D, ONCE>(s, q, lg);
   const uint32_t total = uniform_u32(d.total);
   if (blockIdx.x == 0 && threadIdx.x < kMaxRowSeqs) {   // what the join needs of it
@@ -457,6 +455,7 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     fetch_pages(b0);
     request(b0, 0);
     fetch_pages(min(b0 + 1u, b1 - 1u));
+    if (TREE && b1 * kBlockKeys > pos0) tree_bits(a.parents + begin, T, seq, s.err, bits, reach);
     // ---- queries: B operand, lane = row, 8 columns a step and half
     const uint32_t r = tile * kTileRows + wave * 32u + l31, rr = min(r, rows - 1u), t = rr >> lg;
     const uint32_t head = (kvh << lg) + (rr & ((1u << lg) - 1u)), pos = pos0 + t;
@@ -493,7 +492,8 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
       }
       const uint32_t kt = lds0 + buf * 2u * TILE, vt = kt + TILE;
       bool poisoned = false;
-      if (kv0 + kBlockKeys - 1u > tile_lo) {   // some row does not see all of the block
+      const bool in_tree = TREE && kv0 + kBlockKeys > pos0;
+      if (TREE ? in_tree : kv0 + kBlockKeys - 1u > tile_lo) {   // some row does not see all of the block
         // 0 x NaN is NaN: a value that is not finite must not meet the zero probability of a row that does not see it.  Such
         // values are taken out of the tile and added below to the rows that do.
         lds_u32* p = (lds_u32*)(uintptr_t)(vt + threadIdx.x * (TILE / 256u));
@@ -536,7 +536,15 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         }
         __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
         __builtin_amdgcn_s_setprio(1);
-        if (kv0 + kBlockKeys - 1u > pos_lo) {
+        if (TREE && in_tree) {
+          const uint64_t w = bits_from(bits + t * (kTreeNodes / 64u), (int32_t)(kv0 - pos0)) >> (4u * half);
+          const uint32_t lo = (uint32_t)w, hi = (uint32_t)(w >> 32);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[n][i] = (n ? hi : lo) & (1u << (8 * (i >> 2) + (i & 3))) ? sc[n][i] : -INFINITY;
+        }
+        if (!TREE && kv0 + kBlockKeys - 1u > pos_lo) {
           const int32_t seen = (int32_t)(pos - kv0 - 4u * half);
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -590,7 +598,8 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
         if (__builtin_expect(poisoned, 0)) {
           for (uint32_t j = 0; j < kBlockKeys && kv0 + j <= pos_hi; ++j) {
             size_t at = 0;
-            if (!cache_row(s, slot, kvh, kv0 + j, &at) || kv0 + j > pos) continue;
+            if (!cache_row(s, slot, kvh, kv0 + j, &at)) continue;
+            if (TREE ? !(bits_from(bits + t * (kTreeNodes / 64u), (int32_t)(kv0 - pos0)) >> j & 1u) : kv0 + j > pos) continue;
 #pragma unroll
             for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
@@ -633,6 +642,11 @@ __global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint3
     }
   }
 }
+
+template <int D, bool PAGED, bool ONCE>
+__global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) { attend_units<D, PAGED, ONCE, false>(a, lg); }
+template <int D, bool PAGED, bool ONCE>
+__global__ void __launch_bounds__(256, 2) tree_attend_kernel(AttendArgs a, uint32_t lg) { attend_units<D, PAGED, ONCE, true>(a, lg); }
 
 // Joins the partial results of a row whose tile was cut into runs, in their order: W wavefronts per row and query head, every W-th
 // run each.
@@ -718,7 +732,6 @@ __global__ void __launch_bounds__(256) rows_attend_join_kernel(AttendArgs a, uin
   }
 }
 
-constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
 hipError_t rows_prepare(int device) {
   static std::mutex mu;
   static std::vector<bool> done;
@@ -728,6 +741,9 @@ hipError_t rows_prepare(int device) {
   for (const void* fn : {(const void*)rows_attend_kernel<128, false, false>, (const void*)rows_attend_kernel<128, true, false>,
                          (const void*)rows_attend_kernel<128, false, true>, (const void*)rows_attend_kernel<128, true, true>})
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_lds(128));
+  for (const void* fn : {(const void*)tree_attend_kernel<128, false, false>, (const void*)tree_attend_kernel<128, true, false>,
+                         (const void*)tree_attend_kernel<128, false, true>, (const void*)tree_attend_kernel<128, true, true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tree_attend_lds(128));
   if (e == hipSuccess) {
     done.resize(std::max(done.size(), (size_t)device + 1u));
     done[device] = true;
@@ -735,8 +751,13 @@ hipError_t rows_prepare(int device) {
   return e;
 }
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool TREE>
 static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t stream) {
+  auto run = [&](uint32_t grid, auto once) {
+    constexpr bool ONCE = decltype(once)::value;
+    if constexpr (TREE) tree_attend_kernel<D, PAGED, ONCE><<<dim3(grid), dim3(256), tree_attend_lds(D), stream>>>(a, lg);
+    else rows_attend_kernel<D, PAGED, ONCE><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+  };
   // units: one per tile, and up to kAttendSlots more where tiles are cut (a workgroup without one has worked that out for nothing;
   // one takes several where there are more)
   const uint64_t tiles = (((uint64_t)a.s.n_rows << lg) / kTileRows + a.s.n_seqs) * a.s.n_kv;
@@ -748,9 +769,9 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   // 26.0 / 27.8 us; 16 x 2 / 16 x 3 over 2000, heads of 64, 15.3 / 19.0).
   if (a.s.n_rows << lg <= kTileRows) {
     const uint32_t runs = std::min(kAttendFewChunks, a.s.max_seq / (kAttendMinBlocks * kBlockKeys) + 1u);
-    rows_attend_kernel<D, PAGED, true><<<dim3(std::min(attend_slots(D, true), a.s.n_seqs * a.s.n_kv * runs)), dim3(256), attend_lds(D), stream>>>(a, lg);
+    run(std::min(attend_slots(D, true), a.s.n_seqs * a.s.n_kv * runs), std::true_type());
   }
-  else rows_attend_kernel<D, PAGED, false><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+  else run(grid, std::false_type());
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.s.max_seq < (kAttendMinBlocks + kAttendJoinBlocks) * kBlockKeys) return e;   // (never cut)
   // On a longer cache the host cannot tell whether anything was cut, so a call that was not pays for the launch (64 tokens, max_seq 64 / 4096:
@@ -760,11 +781,15 @@ static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t st
   else rows_attend_join_kernel<D, 1><<<dim3((uint32_t)std::min<uint64_t>((items + 3u) / 4u, kJoinWorkgroups)), dim3(256), 0, stream>>>(a, lg);
   return hipGetLastError();
 }
-hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
+template <bool TREE>
+static hipError_t launch_attend(const AttendArgs& a, hipStream_t stream) {
   uint32_t lg = 0;
   while ((1u << lg) < a.s.n_q / a.s.n_kv) ++lg;
-  if (a.s.head_dim == 128u) return a.s.table ? launch_attend<128, true>(a, lg, stream) : launch_attend<128, false>(a, lg, stream);
-  return a.s.table ? launch_attend<64, true>(a, lg, stream) : launch_attend<64, false>(a, lg, stream);
+  if (a.s.head_dim == 128u) return a.s.table ? launch_attend<128, true, TREE>(a, lg, stream) : launch_attend<128, false, TREE>(a, lg, stream);
+  return a.s.table ? launch_attend<64, true, TREE>(a, lg, stream) : launch_attend<64, false, TREE>(a, lg, stream);
+}
+hipError_t launch_rows_attend(const AttendArgs& a, hipStream_t stream) {
+  return a.parents ? launch_attend<true>(a, stream) : launch_attend<false>(a, stream);
 }
 
 // ------------------------------------------------------------------------------------ log probabilities

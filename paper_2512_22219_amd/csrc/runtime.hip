@@ -713,6 +713,21 @@ extern "C" mpk_status mpk_graph_status(mpk_graph* g) {
     case DE_BAD_SLOT:
       set_error("sequence %u has slot %d, outside [0, batch) or an earlier sequence's", err[2], (int)err[3]);
       return MPK_ERR_DEVICE;
+    case DE_BAD_PARENT:
+      set_error("sequence %u: node %u of its tree has no earlier node for a parent (or is a second root)", err[2], err[3]);
+      return MPK_ERR_DEVICE;
+    case DE_BAD_TREE:
+      set_error("sequence %u has a tree of %u nodes, at most %u are possible", err[2], err[3], MPK_TREE_MAX_NODES);
+      return MPK_ERR_DEVICE;
+    case DE_BAD_TEMPERATURE: {
+      float t;
+      memcpy(&t, &err[3], sizeof t);
+      set_error("sequence %u has the temperature %g, which is negative or not finite", err[2], (double)t);
+      return MPK_ERR_DEVICE;
+    }
+    case DE_BAD_PATH:
+      set_error("sequence %u: place %u of its path, or its length, does not fit its tree", err[2], err[3]);
+      return MPK_ERR_DEVICE;
     default: set_error("unknown device error %u", err[0]); return MPK_ERR_DEVICE;
   }
 }
@@ -1119,7 +1134,7 @@ extern "C" void mpk_serve_destroy(mpk_server* s) {
 
 // ------------------------------------------------------------------ rows beside the decode step
 // Arguments are looked at first, whether the graph can run anything last: what a call refuses can be tried without a GPU.
-// Buffers of no rows are not looked at: an empty tensor has no address.
+// Buffers of no rows are not looked at: an empty tensor has no address.  Calls on trees are calls on rows that have parents.
 static mpk_status rows_runnable(const mpk_graph* g) {
   if (g->h.opt.serving) { set_error("a serving graph's slots and pages belong to its server"); return MPK_ERR_INVALID_ARG; }
   if (g->host_only) { set_error("graph was compiled host_only"); return MPK_ERR_INVALID_ARG; }
@@ -1147,6 +1162,9 @@ static mpk_status rows_count(uint32_t n_rows) {
   if (n_rows > kRowsMost) { set_error("n_rows %u is above %u", n_rows, kRowsMost); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
 }
+static size_t rows_of_layer(const HostGraph& h) {   // cache rows of one layer and KV head
+  return h.opt.kv_page_size ? (size_t)h.opt.kv_pages * h.opt.kv_page_size : (size_t)(h.opt.kv_batch ? h.opt.kv_batch : h.cfg.batch) * h.cfg.max_seq;
+}
 static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
                             const int32_t* slots, const int32_t* positions, RowSeqs* s) {
   if (!g || !row_begin || !positions) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
@@ -1166,15 +1184,13 @@ static mpk_status rows_seqs(const mpk_graph* g, uint32_t layer, uint32_t n_seqs,
   s->n_q = h.cfg.n_q_heads; s->n_kv = h.cfg.n_kv_heads; s->head_dim = h.cfg.head_dim;
   s->batch = h.cfg.batch; s->max_seq = h.cfg.max_seq;
   s->err = g->d_err;
-  size_t rows = (size_t)(h.opt.kv_batch ? h.opt.kv_batch : h.cfg.batch) * h.cfg.max_seq;   // of one layer and KV head
   if (h.opt.kv_page_size) {
     s->table = g->page_table;
     s->n_pages = h.opt.kv_pages;
     s->blocks = h.cfg.max_seq / h.opt.kv_page_size;
     while ((1u << s->page_shift) < h.opt.kv_page_size) ++s->page_shift;
-    rows = (size_t)h.opt.kv_pages * h.opt.kv_page_size;
   }
-  const size_t at = (size_t)layer * rows * s->n_kv * s->head_dim;
+  const size_t at = (size_t)layer * rows_of_layer(h) * s->n_kv * s->head_dim;
   if (g->cache_k) { s->k = g->cache_k + at; s->v = g->cache_v + at; }
   return MPK_OK;
 }
@@ -1184,24 +1200,61 @@ static mpk_status rows_cache_runnable(const mpk_graph* g) {
   return st;
 }
 
+static mpk_status rows_parents(const int32_t* parents, const int32_t** out) {
+  if (!parents) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  *out = parents;
+  return rows_words("parents", parents);
+}
+
+static mpk_status append_rows(mpk_graph* g, uint32_t layer, AppendArgs* a, const void* qkv, uint32_t qkv_type, size_t qkv_stride,
+                              void* q_out, size_t q_stride, void* stream) {
+  mpk_status st;
+  if (qkv_type > MPK_ROWS_F32) { set_error("unknown qkv_type %u", qkv_type); return MPK_ERR_INVALID_ARG; }
+  const size_t q = (size_t)a->s.n_q * a->s.head_dim;
+  if (!a->s.n_rows) return rows_cache_runnable(g);
+  if ((st = rows_buffer("qkv", qkv, qkv_stride, q + 2 * (size_t)a->s.n_kv * a->s.head_dim)) != MPK_OK) return st;
+  if ((st = rows_buffer("q_out", q_out, q_stride, q)) != MPK_OK) return st;
+  if (qkv == q_out && (qkv_type != MPK_ROWS_BF16 || qkv_stride != q_stride)) { set_error("queries are rotated in place in bf16 rows of one stride only"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
+  a->qkv = qkv; a->qkv_stride = qkv_stride;
+  a->q_out = (uint16_t*)q_out; a->q_stride = q_stride;
+  a->q_norm = g->qk_gains[layer].first; a->k_norm = g->qk_gains[layer].second;
+  a->inv_freq = g->d_inv_freq; a->eps = g->h.cfg.rms_eps;
+  HIP_TRY(launch_rows_append(*a, qkv_type == MPK_ROWS_F32, (hipStream_t)stream));
+  return MPK_OK;
+}
+
 extern "C" mpk_status mpk_rows_append(mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
                                       const int32_t* slots, const int32_t* positions, const void* qkv, uint32_t qkv_type,
                                       size_t qkv_stride, void* q_out, size_t q_stride, void* stream) {
   AppendArgs a{};
+  const mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
+  return st != MPK_OK ? st : append_rows(g, layer, &a, qkv, qkv_type, qkv_stride, q_out, q_stride, stream);
+}
+
+extern "C" mpk_status mpk_tree_append(mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
+                                      const int32_t* slots, const int32_t* positions, const int32_t* parents, const void* qkv,
+                                      uint32_t qkv_type, size_t qkv_stride, void* q_out, size_t q_stride, void* stream) {
+  AppendArgs a{};
   mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
-  if (st != MPK_OK) return st;
-  if (qkv_type > MPK_ROWS_F32) { set_error("unknown qkv_type %u", qkv_type); return MPK_ERR_INVALID_ARG; }
-  const size_t q = (size_t)a.s.n_q * a.s.head_dim;
-  if (!n_rows) return rows_cache_runnable(g);
-  if ((st = rows_buffer("qkv", qkv, qkv_stride, q + 2 * (size_t)a.s.n_kv * a.s.head_dim)) != MPK_OK) return st;
-  if ((st = rows_buffer("q_out", q_out, q_stride, q)) != MPK_OK) return st;
-  if (qkv == q_out && (qkv_type != MPK_ROWS_BF16 || qkv_stride != q_stride)) { set_error("queries are rotated in place in bf16 rows of one stride only"); return MPK_ERR_INVALID_ARG; }
+  if (st == MPK_OK && n_rows) st = rows_parents(parents, &a.parents);
+  return st != MPK_OK ? st : append_rows(g, layer, &a, qkv, qkv_type, qkv_stride, q_out, q_stride, stream);
+}
+
+static mpk_status attend_rows(mpk_graph* g, AttendArgs* a, const void* q, size_t q_stride, void* out, size_t out_stride,
+                              void* workspace, void* stream) {
+  mpk_status st;
+  if (!a->s.n_rows) return rows_cache_runnable(g);
+  const size_t width = (size_t)a->s.n_q * a->s.head_dim;
+  if ((st = rows_buffer("q", q, q_stride, width)) != MPK_OK) return st;
+  if ((st = rows_buffer("out", out, out_stride, width)) != MPK_OK) return st;
+  if (q == out) { set_error("out is q"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_work(workspace)) != MPK_OK) return st;
   if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
-  a.qkv = qkv; a.qkv_stride = qkv_stride;
-  a.q_out = (uint16_t*)q_out; a.q_stride = q_stride;
-  a.q_norm = g->qk_gains[layer].first; a.k_norm = g->qk_gains[layer].second;
-  a.inv_freq = g->d_inv_freq; a.eps = g->h.cfg.rms_eps;
-  HIP_TRY(launch_rows_append(a, qkv_type == MPK_ROWS_F32, (hipStream_t)stream));
+  a->q = (const uint16_t*)q; a->q_stride = q_stride;
+  a->out = (uint16_t*)out; a->out_stride = out_stride;
+  a->work = workspace;
+  HIP_TRY(launch_rows_attend(*a, (hipStream_t)stream));
   return MPK_OK;
 }
 
@@ -1209,20 +1262,17 @@ extern "C" mpk_status mpk_rows_attend(mpk_graph* g, uint32_t layer, uint32_t n_s
                                       const int32_t* slots, const int32_t* positions, const void* q, size_t q_stride, void* out,
                                       size_t out_stride, void* workspace, void* stream) {
   AttendArgs a{};
+  const mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
+  return st != MPK_OK ? st : attend_rows(g, &a, q, q_stride, out, out_stride, workspace, stream);
+}
+
+extern "C" mpk_status mpk_tree_attend(mpk_graph* g, uint32_t layer, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin,
+                                      const int32_t* slots, const int32_t* positions, const int32_t* parents, const void* q,
+                                      size_t q_stride, void* out, size_t out_stride, void* workspace, void* stream) {
+  AttendArgs a{};
   mpk_status st = rows_seqs(g, layer, n_seqs, n_rows, row_begin, slots, positions, &a.s);
-  if (st != MPK_OK) return st;
-  if (!n_rows) return rows_cache_runnable(g);
-  const size_t width = (size_t)a.s.n_q * a.s.head_dim;
-  if ((st = rows_buffer("q", q, q_stride, width)) != MPK_OK) return st;
-  if ((st = rows_buffer("out", out, out_stride, width)) != MPK_OK) return st;
-  if (q == out) { set_error("out is q"); return MPK_ERR_INVALID_ARG; }
-  if ((st = rows_work(workspace)) != MPK_OK) return st;
-  if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
-  a.q = (const uint16_t*)q; a.q_stride = q_stride;
-  a.out = (uint16_t*)out; a.out_stride = out_stride;
-  a.work = workspace;
-  HIP_TRY(launch_rows_attend(a, (hipStream_t)stream));
-  return MPK_OK;
+  if (st == MPK_OK && n_rows) st = rows_parents(parents, &a.parents);
+  return st != MPK_OK ? st : attend_rows(g, &a, q, q_stride, out, out_stride, workspace, stream);
 }
 
 extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const void* logits, uint32_t logits_type, size_t row_stride,
@@ -1251,6 +1301,64 @@ extern "C" mpk_status mpk_rows_logprobs(mpk_graph* g, uint32_t n_rows, const voi
   a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
   a.work = workspace; a.err = g->d_err; a.arrivals = g->d_arrivals;
   HIP_TRY(launch_rows_logprobs(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
+  return MPK_OK;
+}
+
+extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin, const int32_t* parents,
+                                      const int32_t* tokens, const void* logits, uint32_t logits_type, size_t row_stride,
+                                      const float* draft_probs, size_t draft_stride, uint32_t flags, const float* temperatures,
+                                      const float* uniforms, int32_t* lengths, int32_t* path, int32_t* next_tokens, float* logprobs,
+                                      void* workspace, void* stream) {
+  if (!g || !row_begin || !lengths || !next_tokens) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  const HostGraph& h = g->h;
+  if (!h.cfg.vocab) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
+  const uint32_t vocab = h.cfg.vocab;
+  if (n_seqs == 0 || n_seqs > std::min(h.cfg.batch, kMaxRowSeqs)) { set_error("n_seqs %u is outside 1..%u, the graph's batch", n_seqs, h.cfg.batch); return MPK_ERR_INVALID_ARG; }
+  if (logits_type > MPK_ROWS_F32) { set_error("unknown logits_type %u", logits_type); return MPK_ERR_INVALID_ARG; }
+  if (flags & ~MPK_TREE_DRAWN_ONCE) { set_error("unknown flags bits"); return MPK_ERR_INVALID_ARG; }
+  if (flags && !draft_probs && n_rows) { set_error("MPK_TREE_DRAWN_ONCE without draft_probs"); return MPK_ERR_INVALID_ARG; }
+  mpk_status st = rows_count(n_rows);
+  if (st != MPK_OK) return st;
+  const std::pair<const char*, const void*> words[] = {{"row_begin", row_begin}, {"temperatures", temperatures}, {"lengths", lengths}, {"next_tokens", next_tokens}};
+  for (const auto& w : words)
+    if ((st = rows_words(w.first, w.second)) != MPK_OK) return st;
+  if (n_rows) {
+    if (!parents || !tokens || !path || (temperatures && !uniforms)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+    const std::pair<const char*, const void*> lists[] = {{"parents", parents}, {"tokens", tokens}, {"uniforms", uniforms}, {"path", path},
+                                                         {"logprobs", logprobs}, {"draft_probs", draft_probs}};
+    for (const auto& w : lists)
+      if ((st = rows_words(w.first, w.second)) != MPK_OK) return st;
+    if (!logits || (uintptr_t)logits % (logits_type == MPK_ROWS_F32 ? 4 : 2)) { set_error("logits is NULL or not aligned to its elements"); return MPK_ERR_INVALID_ARG; }
+    if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
+    if (draft_probs && draft_stride < vocab) { set_error("draft_probs: a row stride of %zu elements, the vocabulary has %u", draft_stride, vocab); return MPK_ERR_INVALID_ARG; }
+    if ((st = rows_work(workspace)) != MPK_OK) return st;
+  }
+  if ((st = rows_runnable(g)) != MPK_OK) return st;
+  VerifyArgs a{};
+  a.row_begin = row_begin; a.parents = parents; a.tokens = tokens;
+  a.n_seqs = n_seqs; a.n_rows = n_rows; a.vocab = vocab; a.flags = flags;
+  a.logits = logits; a.stride = row_stride; a.draft = draft_probs; a.draft_stride = draft_stride;
+  a.temperatures = temperatures; a.uniforms = uniforms;
+  a.lengths = lengths; a.path = path; a.next = next_tokens; a.logprobs = logprobs;
+  a.work = workspace; a.err = g->d_err;
+  HIP_TRY(launch_tree_verify(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
+  return MPK_OK;
+}
+
+extern "C" mpk_status mpk_tree_keep(mpk_graph* g, uint32_t n_seqs, uint32_t n_rows, const int32_t* row_begin, const int32_t* slots,
+                                    const int32_t* positions, const int32_t* lengths, const int32_t* path, int32_t* positions_out,
+                                    void* stream) {
+  KeepArgs a{};
+  mpk_status st = rows_seqs(g, 0, n_seqs, n_rows, row_begin, slots, positions, &a.s);
+  if (st != MPK_OK) return st;
+  if (n_rows && (!lengths || !path)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_words("lengths", lengths)) != MPK_OK || (st = rows_words("path", path)) != MPK_OK || (st = rows_words("positions_out", positions_out)) != MPK_OK) return st;
+  if (positions_out == positions) { set_error("positions_out is positions"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
+  a.n_layers = g->h.cfg.n_layers;
+  a.layer_stride = rows_of_layer(g->h) * a.s.n_kv * a.s.head_dim;
+  a.lengths = lengths; a.path = path; a.positions_out = positions_out;
+  HIP_TRY(launch_tree_keep(a, (hipStream_t)stream));
   return MPK_OK;
 }
 

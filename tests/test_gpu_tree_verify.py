@@ -1,0 +1,350 @@
+"""mpk_tree_verify on the GPU against the definition in 64 bits."""
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2512_22219_amd as M
+from tests.tree_util import F32_HALF, TreeModel, tree, verify_exact, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+def _begin(lens, first=0):
+    out = [first]
+    for n in lens:
+        out.append(out[-1] + n)
+    return out
+
+
+def _tokens(gen, logits, parents, begin, draft, once, temperatures):
+    """Tokens that the walk has something to do with: near the top of the parent's row, or drawn from the draft's."""
+    tokens = [0] * logits.shape[0]
+    for i in range(len(begin) - 1):
+        seen = {}
+        for t in range(begin[i], begin[i + 1]):
+            p = parents[t]
+            if p < 0:
+                continue
+            row = begin[i] + p
+            j = seen[p] = seen.get(p, -1) + 1
+            if draft is not None:
+                q = draft[row].double().clone()
+                for u in range(begin[i], t):
+                    if once and parents[u] == p:
+                        q[tokens[u]] = 0
+                tokens[t] = int(torch.multinomial(q, 1, generator=gen)) if q.sum() > 0 else 0
+            else:
+                tokens[t] = int(logits[row].float().nan_to_num(-1e30).topk(min(j + 1, logits.shape[1])).indices[-1])
+    return tokens
+
+
+def _check(m, begin, parents, tokens, logits, out, temperatures, uniforms, draft=None, once=False, work=None):
+    lengths, path, nxt, lp = (t.cpu() for t in out)
+    mine = torch.zeros(len(path), dtype=torch.bool)
+    for i in range(len(begin) - 1):
+        r = slice(begin[i], begin[i + 1])
+        mine[r] = True
+        if begin[i] == begin[i + 1]:
+            assert int(lengths[i]) == 0 and int(nxt[i]) == -1
+            continue
+        walk, token, logs = verify_exact(parents[r], tokens[r], logits[r], temperatures[i] if temperatures is not None else 0.0,
+                                         [0.0] * (r.stop - r.start) if uniforms is None else uniforms[r].tolist(), None if draft is None else draft[r], once)
+        rest = r.stop - r.start - len(walk)
+        assert int(lengths[i]) == len(walk) and path[r].tolist() == walk + [-1] * rest and int(nxt[i]) == token, i
+        want = torch.tensor(logs + [0.0] * rest, dtype=torch.float64)
+        # 64-bit sums to 1e-9 or better, one rounding to 32 bits
+        far = (lp[r].double() - want).abs() - (F32_HALF * want.abs() + 2e-9)
+        assert (torch.isnan(want) == torch.isnan(lp[r])).all() and not (far > 0).any(), (i, float(far.max()))
+    assert (path[~mine] == 77).all() and (lp[~mine] == 77).all()
+
+
+def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperatures=None, first=0, behind=0, pad=0, std=2.0, batch=16, masked=0.0):
+    gen = torch.Generator().manual_seed(seed)
+    m = TreeModel(n_q=2, n_kv=1, batch=batch, max_seq=8, vocab=vocab, layers=1)
+    begin = _begin(lens, first)
+    rows = begin[-1] + behind
+    parents = [55] * first + sum((tree(n, k, seed + i) for i, (n, k) in enumerate(zip(lens, kinds))), []) + [-55] * behind
+    x = torch.randn(rows, vocab, generator=gen) * std
+    up = torch.randint(vocab, (rows,), generator=gen)
+    x[torch.arange(rows), up] += 8 * torch.rand(rows, generator=gen)
+    if masked:
+        gone = torch.rand(rows, vocab, generator=gen) < masked
+        gone[torch.arange(rows), up] = False
+        x[gone] = -math.inf
+    logits = x.to(dtype)
+    q = None
+    if draft:
+        q = torch.softmax((logits.float() + torch.randn(rows, vocab, generator=gen)) / 1.2, 1)
+    once = draft == "once"
+    tokens = _tokens(gen, logits, parents, begin, q, once, temperatures)
+    uniforms = torch.rand(rows, generator=gen)
+    if temperatures is None:
+        temps = None
+    else:
+        temps = [temperatures[i % len(temperatures)] for i in range(len(lens))]
+    dev = torch.device("cuda")
+    wide = torch.full((rows, vocab + pad), float("nan"), dtype=dtype, device=dev)
+    wide[:, :vocab] = logits.to(dev)
+    dwide = None
+    if q is not None:
+        dwide = torch.full((rows, vocab + pad), float("nan"), device=dev)
+        dwide[:, :vocab] = q.to(dev)
+    out = m.verify(begin, parents, tokens, wide, workspace(), draft=dwide, once=once, temperatures=temps, uniforms=None if temps is None else uniforms)
+    m.status()
+    _check(m, begin, parents, tokens, logits, out, temps, uniforms, q, once)
+    return out
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("draft", [None, "drawn", "once"])
+@pytest.mark.parametrize("vocab,pad", [(1, 0), (2, 1), (63, 0), (64, 3), (257, 0), (1000, 8), (4097, 1), (33001, 7)])
+def test_verify(vocab, pad, draft, dtype):
+    _case(vocab, vocab, [1, 0, 2, 9, 40, 17, 5, 6], ["chain", "chain", "chain", "star", "random", "two", "star", "chain"], dtype, draft,
+          [1.0, 0.6, 0.0, 1.3, 1.0, 0.9, 1.7, 1.0], first=2, behind=1, pad=pad)
+
+
+@pytest.mark.parametrize("draft", [None, "drawn", "once"])
+@pytest.mark.parametrize("temperatures", [None, [0.0], [1.0], [0.25, 4.0]])
+def test_verify_at_a_large_vocabulary(draft, temperatures):
+    _case(3, 151936, [8, 1, 5], ["random", "chain", "star"], torch.bfloat16, draft, temperatures)
+
+
+@pytest.mark.parametrize("draft", [None, "once"])
+@pytest.mark.parametrize("kind", ["chain", "star", "random"])
+def test_verify_the_largest_trees(kind, draft):
+    _case(7, 300, [256, 255, 1], [kind] * 3, torch.float32, draft, [1.0, 0.0, 1.0])
+
+
+@pytest.mark.parametrize("draft", [None, "drawn"])
+@pytest.mark.parametrize("std", [0.0, 0.01, 30.0, 3000.0, 1e30])
+def test_verify_flat_and_peaked_rows(std, draft):
+    _case(11, 5000, [6, 20, 3], ["chain", "random", "star"], torch.float32, draft, [1.0, 0.5, 2.0], std=std)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("masked", [0.5, 0.999, 1.0])
+def test_verify_under_a_grammar(masked, dtype):
+    """Most tokens, or all but one, are ruled out."""
+    out = _case(5, 3001, [6, 20, 3, 9], ["chain", "random", "star", "two"], dtype, None, [1.0, 0.5, 0.0, 1.0], masked=masked)
+    assert (out[2] >= 0).all()
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_verifications(seed):
+    rng = random.Random(seed)
+    n = rng.choice([1, 2, 5, 16])
+    lens = [rng.choice([0, 1, rng.randint(1, 10), rng.randint(1, 60)]) for _ in range(n)]
+    _case(seed, rng.choice([17, 128, 999, 4096, 20011]), lens, [rng.choice(["chain", "star", "two", "random"]) for _ in lens],
+          rng.choice([torch.float32, torch.bfloat16]), rng.choice([None, None, "drawn", "once"]), rng.choice([None, [0.0, 1.0], [1.0], [0.7, 1.1]]),
+          first=rng.choice([0, 1]), behind=rng.choice([0, 4]), pad=rng.choice([0, 0, 1, 5, 8]), masked=rng.choice([0.0, 0.0, 0.8]))
+
+
+@pytest.mark.parametrize("draft", [None, "drawn", "once"])
+def test_the_tokens_have_the_targets_distribution(draft):
+    """The first two tokens behind the root, over many uniform numbers, against p(a) p(b | a): trees over a vocabulary of four, where
+    a tree holds every token's continuation, so that p(b | a) is the same whichever way a came about."""
+    V, S, calls, temp = 4, 16, 120, 0.8
+    m = TreeModel(n_q=2, n_kv=1, batch=S, max_seq=8, vocab=V, layers=1)
+    gen = torch.Generator().manual_seed(9)
+    logit_of = torch.randn(V, V, generator=gen) * 1.5       # row: the token in front
+    root_logits, guess = torch.randn(V, generator=gen) * 1.5, torch.randn(V + 1, V, generator=gen)
+    q_root, q_of = torch.softmax(guess[V], 0), torch.softmax(guess[:V], 1)
+    work, counts, drawn_gen = workspace(), torch.zeros(V, V), torch.Generator().manual_seed(10)
+    for _ in range(calls):
+        parents, tokens, rows, qs = [], [], [], []
+        for _ in range(S):
+            # three children of the root (chosen: 2, 0, 2 again), two of each of these
+            if draft is None:
+                first, second = [2, 0, 2], lambda a: [1, 3]  # noqa: E731
+            else:
+                first = torch.multinomial(q_root, 3, replacement=draft == "drawn", generator=drawn_gen).tolist()
+                second = lambda a: torch.multinomial(q_of[a], 2, replacement=draft == "drawn", generator=drawn_gen).tolist()  # noqa: E731
+            parents += [-1, 0, 0, 0] + [1, 1, 2, 2, 3, 3]
+            below = [x for a in first for x in second(a)]
+            tokens += [0] + first + below
+            rows += [root_logits] + [logit_of[a] for a in first + below]
+            qs += [q_root] + [q_of[a] for a in first + below]
+        n = len(parents)
+        logits, u = torch.stack(rows).cuda(), torch.rand(n, generator=gen)
+        lengths, path, nxt, _ = (t.cpu() for t in m.verify(list(range(0, n + 1, 10)), parents, tokens, logits, work, torch.stack(qs).cuda() if draft else None,
+                                                             draft == "once", [temp] * S, u))
+        for i in range(S):
+            walk = [tokens[10 * i + t] for t in path[10 * i:10 * i + int(lengths[i])].tolist()[1:]] + [int(nxt[i])]
+            if len(walk) == 1:   # the token behind it is drawn as ever
+                walk.append(int(torch.multinomial(torch.softmax(logit_of[walk[0]] / temp, 0), 1, generator=gen)))
+            counts[walk[0], walk[1]] += 1
+    m.status()
+    p = torch.softmax(root_logits / temp, 0)[:, None] * torch.softmax(logit_of / temp, 1)
+    total = S * calls
+    # a count is binomial: five standard deviations, and one for the smallest
+    assert ((counts - total * p).abs() <= 5 * (total * p * (1 - p)).sqrt() + 1).all(), (counts, total * p)
+
+
+def test_numbers_on_the_edge():
+    """u = 0 accepts whatever has any probability and draws the first token that has; the largest number below 1 draws the last."""
+    V = 700
+    m = TreeModel(n_q=2, n_kv=1, batch=16, max_seq=8, vocab=V, layers=1)
+    x = torch.full((6, V), -math.inf)
+    x[:, 5:650] = 0.0
+    x[0, 9] = -200.0
+    work, below_one = workspace(), 1 - 2 ** -24
+    parents, tokens = [-1, 0, 1, -1, 0, 1], [0, 9, 4, 0, 700, 9]
+    for u, want in (([0.0, 0.0, 0.0], [2, 2, 5]), ([below_one, 0.0, 0.0], [2, 2, 649]), ([below_one, 1e-3, 0.0], [1, 1, 649])):
+        out = m.verify([0, 3], parents[:3], tokens[:3], x[:3].cuda(), work, temperatures=[1.0], uniforms=u)
+        m.status()
+        # node 1 (token 9: e^-200) is accepted at u = 0 alone, node 2 (token 4: ruled out) never
+        assert [int(out[0][0]), len([t for t in out[1].tolist() if t >= 0]), int(out[2][0])] == want
+
+
+def test_rows_without_a_distribution_end_the_walk():
+    V = 1000
+    m = TreeModel(n_q=2, n_kv=1, batch=16, max_seq=8, vocab=V, layers=1)
+    work = workspace()
+    for dtype in (torch.float32, torch.bfloat16):
+        for bad in (math.nan, math.inf, None):
+            x = torch.randn(8, V)
+            x[0, 7] = 40.0
+            if bad is None:
+                x[1] = -math.inf
+            else:
+                x[1, 999] = bad
+            x[5, 0] = math.nan   # (a node that the walk does not come to)
+            for temp in (0.0, 1.0):
+                out = m.verify([0, 4, 8], [-1, 0, 1, 2, -1, 0, 0, 0], [0, 7, 1, 1, 0, 1, 2, 3], x.to(dtype).cuda(), work, temperatures=[temp, 0.0],
+                               uniforms=[0.5] * 8)
+                m.status()
+                assert out[0].tolist()[0] == 2 and out[1].tolist()[:4] == [0, 1, -1, -1] and int(out[2][0]) == -1
+                lp = out[3].tolist()
+                assert math.isfinite(lp[0]) and math.isnan(lp[1]) and lp[2:4] == [0.0, 0.0] and int(out[2][1]) >= 0
+
+
+def test_a_draft_that_knows_no_other_token():
+    """Draft and target agree on one token, the draft's only one; and a draft whose tokens are all drawn: nothing is left to subtract."""
+    V = 64
+    m = TreeModel(n_q=2, n_kv=1, batch=16, max_seq=8, vocab=V, layers=1)
+    x, q, work = torch.full((4, V), -math.inf), torch.zeros(4, V), workspace()
+    x[:, 3], q[:, 3] = 0.0, 1.0
+    out = m.verify([0, 4], [-1, 0, 1, 2], [0, 3, 3, 3], x.cuda(), work, q.cuda(), True, [1.0], [0.9] * 4)
+    assert out[0].tolist() == [4] and out[2].tolist() == [3]
+    y = torch.zeros(4, V)
+    y[:, 3] = -5.0
+    for once in (False, True):   # token 3 is refused, its twins have no draft distribution left (once)
+        out = m.verify([0, 4], [-1, 0, 0, 0], [0, 3, 3, 3], y.cuda(), work, q.cuda(), once, [1.0], [0.5] * 4)
+        m.status()
+        path, token, _ = verify_exact([-1, 0, 0, 0], [0, 3, 3, 3], y, 1.0, [0.5] * 4, q, once)
+        assert out[0].tolist() == [1] and path == [0] and out[2].tolist() == [token]
+
+
+WRONG = [
+    (dict(begin=[0, 3, 2, 6]), {0, 1, 2}, "row_begin.*sequence 1"), (dict(begin=[0, 3, 4, 7]), {0, 1, 2}, "row_begin.*sequence 2"),
+    (dict(parents=[0, 0, 0, -1, -1, 0]), {0}, "sequence 0: node 0"), (dict(parents=[-1, 0, 2, -1, -1, 0]), {0}, "sequence 0: node 2"),
+    (dict(parents=[-1, 0, -1, -1, -1, 0]), {0}, "sequence 0: node 2"), (dict(parents=[-1, 0, 0, -1, -1, -2]), {2}, "sequence 2: node 1"),
+    (dict(temperatures=[1.0, -1.0, 1.0]), {1}, "sequence 1 has the temperature -1"), (dict(temperatures=[1.0, 1.0, math.nan]), {2}, "sequence 2 has the temperature"),
+    (dict(temperatures=[math.inf, 1.0, 1.0]), {0}, "sequence 0 has the temperature inf"),
+]
+
+
+@pytest.mark.parametrize("change,left,says", WRONG)
+def test_wrong_sequences_are_reported_and_left_out(change, left, says):
+    V = 300
+    m = TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1)
+    args = dict(dict(begin=[0, 3, 4, 6], parents=[-1, 0, 0, -1, -1, 0], temperatures=[1.0, 1.0, 1.0]), **change)
+    x = torch.randn(6, V)
+    out = m.verify(args["begin"], args["parents"], [1, 2, 3, 4, 5, 6], x.cuda(), workspace(), temperatures=args["temperatures"], uniforms=[0.3] * 6)
+    with pytest.raises(M.MpkError, match=says) as e:
+        m.status()
+    assert e.value.status == M.MPK_ERR_DEVICE
+    m.graph.reset()
+    all_out = "row_begin" in says
+    for i in range(3):
+        r = slice(args["begin"][i], args["begin"][i + 1])
+        if i in left:
+            assert int(out[0][i]) == 0 and int(out[2][i]) == -1
+            if not all_out:
+                assert (out[1][r] == -1).all() and (out[3][r] == 0).all()
+        else:
+            path, token, _ = verify_exact(args["parents"][r], [1, 2, 3, 4, 5, 6][r], x[r], 1.0, [0.3] * 6)
+            assert int(out[0][i]) == len(path) and int(out[2][i]) == token
+    if all_out:
+        assert (out[1] == 77).all() and (out[3] == 77).all()
+    # and the next call on the graph is as ever
+    out = m.verify([0, 6], [-1, 0, 0, 1, 2, 2], [1, 2, 3, 4, 5, 6], x.cuda(), workspace(), temperatures=[1.0], uniforms=[0.3] * 6)
+    m.status()
+    path, token, _ = verify_exact([-1, 0, 0, 1, 2, 2], [1, 2, 3, 4, 5, 6], x, 1.0, [0.3] * 6)
+    assert int(out[0][0]) == len(path) and int(out[2][0]) == token
+
+
+def test_a_token_out_of_range_and_a_tree_of_too_many_nodes():
+    V = 300
+    m = TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1)
+    x, work = torch.randn(260, V), workspace()
+    x[0, 8] = 30.0
+    for token in (-1, 300, 2 ** 31 - 1):
+        out = m.verify([0, 3], [-1, 0, 0], [0, token, 8], x[:3].cuda(), work, temperatures=[1.0], uniforms=[0.5] * 3)
+        with pytest.raises(M.MpkError, match=f"sequence 0 has token {token}"):
+            m.status()
+        m.graph.reset()
+        assert out[1].tolist() == [0, 2, -1]   # never accepted; its sibling is
+    out = m.verify([0, 257, 260], [-1] + [0] * 256 + [-1, 0, 0], [8] * 260, x.cuda(), work)
+    with pytest.raises(M.MpkError, match="sequence 0 has a tree of 257 nodes"):
+        m.status()
+    m.graph.reset()
+    assert out[0].tolist()[0] == 0 and int(out[2][0]) == -1 and (out[1][:257] == -1).all() and out[0].tolist()[1] >= 1
+
+
+def test_no_rows_and_no_logprobs():
+    m = TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=100, layers=1)
+    b, n, t = m.ints([0, 0, 0]), m.ints([5, 5]), m.ints([5, 5])
+    m.graph.tree_verify(2, 0, b.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, n.data_ptr(), 0, t.data_ptr(), 0, 0, torch.cuda.current_stream().cuda_stream)
+    m.status()
+    assert n.tolist() == [0, 0] and t.tolist() == [-1, -1]
+    x = torch.randn(5, 100)
+    for temp in (0.0, 1.0):
+        outs = [m.verify([0, 5], [-1, 0, 0, 1, 1], [1, 2, 3, 4, 5], x.cuda(), workspace(), temperatures=[temp], uniforms=[0.4] * 5, logprobs=lp) for lp in (True, False)]
+        m.status()
+        assert all(torch.equal(a, b) for a, b in zip(outs[0][:3], outs[1][:3])) and (outs[1][3] == 77).all()
+
+
+def test_rows_and_strides_far_apart():
+    """Rows whose offsets pass 2^31 elements."""
+    V, stride = 1000, 1 << 30
+    m = TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1)
+    x = torch.randn(5, V).to(torch.bfloat16)
+    far = torch.empty(4 * stride + V, dtype=torch.bfloat16, device="cuda").as_strided((5, V), (stride, 1))
+    far.copy_(x)
+    tokens = [0] + [int(x[p].float().argmax()) for p in (0, 1, 2, 3)]
+    out = m.verify([0, 5], [-1, 0, 1, 2, 3], tokens, far, workspace(), temperatures=[0.01], uniforms=[0.4] * 5)
+    m.status()
+    path, token, _ = verify_exact([-1, 0, 1, 2, 3], tokens, x, 0.01, [0.4] * 5)
+    assert out[1].tolist() == path + [-1] * (5 - len(path)) and int(out[2][0]) == token and len(path) > 2
+
+
+def test_the_same_call_gives_the_same_bits_two_graphs_at_once():
+    """Calls of two graphs on two streams, many at a time, each with its workspace, against one after the other."""
+    V, models = 50000, [TreeModel(n_q=2, n_kv=1, batch=8, max_seq=8, vocab=50000, layers=1) for _ in range(2)]
+    gen, sets = torch.Generator().manual_seed(4), []
+    for m in models:
+        lens = [9, 30, 1, 12]
+        begin, parents = _begin(lens), sum((tree(n, "random", i) for i, n in enumerate(lens)), [])
+        x = (torch.randn(begin[-1], V, generator=gen) * 2).cuda()
+        q = torch.softmax(x + torch.randn(begin[-1], V, generator=gen).cuda(), 1)
+        tokens = _tokens(gen, x.cpu(), parents, begin, q.cpu(), True, None)
+        sets.append((begin, parents, tokens, x, workspace(), q, True, [1.0] * 4, torch.rand(begin[-1], generator=gen)))
+    want = [[t.clone() for t in m.verify(*s)] for m, s in zip(models, sets)]
+    torch.cuda.synchronize()
+    streams, got, keep = [torch.cuda.Stream() for _ in models], [[], []], []
+    outs = [[[torch.empty_like(t).fill_(77) for t in w] for _ in range(20)] for w in want]
+    torch.cuda.synchronize()
+    for k in range(20):
+        for j, (m, s) in enumerate(zip(models, sets)):
+            with torch.cuda.stream(streams[j]):
+                got[j].append(m.verify(*s, stream=streams[j].cuda_stream, out=outs[j][k]))
+                keep.append(m.keep_alive)
+    torch.cuda.synchronize()
+    for m in models:
+        m.status()
+    for g, w in zip(got, want):
+        for out in g:
+            assert all(torch.equal(a, b) for a, b in zip(out, w))

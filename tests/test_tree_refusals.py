@@ -1,0 +1,112 @@
+"""mpk_tree_*: what the entry points refuse, on graphs of the host alone (arguments are looked at before the graph is)."""
+import pytest
+
+import paper_2512_22219_amd as M
+from tests.rows_util import RowsModel
+
+P = 1 << 20   # an aligned address that nothing reads
+
+
+@pytest.fixture(scope="module")
+def model():
+    return RowsModel(batch=3, host_only=True)
+
+
+def _refused(call, *args, match, status=M.MPK_ERR_INVALID_ARG):
+    with pytest.raises(M.MpkError, match=match) as e:
+        call(*args)
+    assert e.value.status == status
+
+
+APPEND = dict(layer=0, n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, parents=P, qkv=P, kind=0, stride=512, q=P + 512, q_stride=256)
+ATTEND = dict(layer=0, n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, parents=P, q=P, q_stride=256, out=P + 512, out_stride=256, work=P)
+VERIFY = dict(n_seqs=1, n_rows=5, begin=P, parents=P, tokens=P, logits=P, kind=1, stride=64, draft=P, draft_stride=64, flags=0,
+              temperatures=P, uniforms=P, lengths=P, path=P, next=P, logprobs=P, work=P)
+KEEP = dict(n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, lengths=P, path=P, out=P + 512)
+
+
+@pytest.mark.parametrize("change,match", [
+    ({}, "host_only"), (dict(n_rows=0, parents=0), "host_only"), (dict(parents=0), "NULL"), (dict(parents=P + 2), "parents"), (dict(layer=2), "layer 2"),
+    (dict(n_seqs=0), "n_seqs 0"), (dict(n_seqs=4), "n_seqs 4"), (dict(n_rows=(1 << 24) + 1), "n_rows"), (dict(begin=0), "NULL"),
+    (dict(positions=0), "NULL"), (dict(qkv=0), "qkv"), (dict(kind=2), "qkv_type"), (dict(stride=504), "qkv"), (dict(q_stride=260), "q_out"),
+    (dict(q=P), "in place"), (dict(q=P, q_stride=512), "host_only")])
+def test_append(model, change, match):
+    _refused(model.graph.tree_append, *dict(APPEND, **change).values(), match=match)
+
+
+@pytest.mark.parametrize("change,match", [
+    ({}, "host_only"), (dict(n_rows=0, parents=0), "host_only"), (dict(parents=0), "NULL"), (dict(parents=P + 1), "parents"), (dict(layer=2), "layer 2"),
+    (dict(n_seqs=4), "n_seqs 4"), (dict(positions=0), "NULL"), (dict(q=P + 8), "q is NULL"), (dict(q_stride=248), "q: "), (dict(out=0), "out"),
+    (dict(out_stride=0), "out"), (dict(out=P), "out is q"), (dict(work=0), "workspace"), (dict(work=P + 4), "workspace")])
+def test_attend(model, change, match):
+    _refused(model.graph.tree_attend, *dict(ATTEND, **change).values(), match=match)
+
+
+@pytest.mark.parametrize("change,match", [
+    ({}, "host_only"), (dict(n_rows=0), "host_only"), (dict(n_seqs=0), "n_seqs 0"), (dict(n_seqs=4), "n_seqs 4"),
+    (dict(n_rows=(1 << 24) + 1), "n_rows"), (dict(begin=0), "NULL"), (dict(parents=0), "NULL"), (dict(tokens=0), "NULL"),
+    (dict(lengths=0), "NULL"), (dict(path=0), "NULL"), (dict(next=0), "NULL"), (dict(logprobs=0), "host_only"), (dict(logits=0), "logits"),
+    (dict(logits=P + 2), "logits"), (dict(logits=P + 2, kind=0), "host_only"), (dict(logits=P + 1, kind=0), "logits"),
+    (dict(kind=2), "logits_type"), (dict(stride=63), "row stride"), (dict(draft_stride=63), "draft_probs"), (dict(draft=P + 2), "draft_probs"),
+    (dict(draft=0, draft_stride=0), "host_only"), (dict(flags=2), "flags"), (dict(flags=1), "host_only"),
+    (dict(flags=1, draft=0), "MPK_TREE_DRAWN_ONCE"), (dict(uniforms=0), "NULL"), (dict(temperatures=0, uniforms=0), "host_only"),
+    (dict(work=0), "workspace"), (dict(work=P + 8), "workspace")])
+def test_verify(model, change, match):
+    _refused(model.graph.tree_verify, *dict(VERIFY, **change).values(), match=match)
+
+
+@pytest.mark.parametrize("change,match", [
+    ({}, "host_only"), (dict(out=0), "host_only"), (dict(out=P), "positions_out is positions"), (dict(n_seqs=0), "n_seqs 0"),
+    (dict(n_seqs=4), "n_seqs 4"), (dict(n_rows=(1 << 24) + 1), "n_rows"), (dict(begin=0), "NULL"), (dict(positions=0), "NULL"),
+    (dict(lengths=0), "NULL"), (dict(path=0), "NULL"), (dict(n_rows=0, lengths=0, path=0), "host_only")])
+def test_keep(model, change, match):
+    _refused(model.graph.tree_keep, *dict(KEEP, **change).values(), match=match)
+
+
+@pytest.mark.parametrize("off", [1, 2])
+@pytest.mark.parametrize("call,args,name,says", [
+    ("tree_append", APPEND, "begin", "row_begin"), ("tree_append", APPEND, "slots", "slots"), ("tree_append", APPEND, "positions", "positions"),
+    ("tree_append", APPEND, "parents", "parents"), ("tree_attend", ATTEND, "parents", "parents"), ("tree_attend", ATTEND, "begin", "row_begin"),
+    ("tree_verify", VERIFY, "begin", "row_begin"), ("tree_verify", VERIFY, "parents", "parents"), ("tree_verify", VERIFY, "tokens", "tokens"),
+    ("tree_verify", VERIFY, "draft", "draft_probs"), ("tree_verify", VERIFY, "temperatures", "temperatures"),
+    ("tree_verify", VERIFY, "uniforms", "uniforms"), ("tree_verify", VERIFY, "lengths", "lengths"), ("tree_verify", VERIFY, "path", "path"),
+    ("tree_verify", VERIFY, "next", "next_tokens"), ("tree_verify", VERIFY, "logprobs", "logprobs"), ("tree_keep", KEEP, "begin", "row_begin"),
+    ("tree_keep", KEEP, "slots", "slots"), ("tree_keep", KEEP, "positions", "positions"), ("tree_keep", KEEP, "lengths", "lengths"),
+    ("tree_keep", KEEP, "path", "path"), ("tree_keep", KEEP, "out", "positions_out")])
+def test_lists_and_results_off_their_elements(model, call, args, name, says, off):
+    assert name in args
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + off}).values(), match=f"^.*{says} is not aligned")
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + 4}).values(), match="host_only")
+
+
+def test_no_rows_need_no_buffers():
+    g = RowsModel(host_only=True).graph
+    for call, args, none in ((g.tree_append, APPEND, ("parents", "qkv", "stride", "q", "q_stride")),
+                             (g.tree_attend, ATTEND, ("parents", "q", "q_stride", "out", "out_stride", "work")),
+                             (g.tree_verify, VERIFY, ("parents", "tokens", "logits", "stride", "draft", "draft_stride", "uniforms", "path", "logprobs", "work")),
+                             (g.tree_keep, KEEP, ("lengths", "path"))):
+        empty = dict(args, n_rows=0, **dict.fromkeys(none, 0))
+        assert list(empty) == list(args)
+        _refused(call, *empty.values(), match="host_only")
+        _refused(call, *dict(empty, n_rows=1).values(), match="NULL")
+        _refused(call, *dict(empty, n_seqs=0).values(), match="n_seqs")
+
+
+def test_a_cache_too_long_for_the_cuts():
+    g = RowsModel(max_seq=(1 << 28) + 8, batch=1, host_only=True).graph
+    for call, args in ((g.tree_append, APPEND), (g.tree_attend, ATTEND), (g.tree_keep, KEEP)):
+        _refused(call, *args.values(), match="max_seq", status=M.MPK_ERR_UNSUPPORTED)
+    _refused(g.tree_verify, *VERIFY.values(), match="host_only")   # (looks at no cache)
+
+
+def test_a_serving_graph_and_a_task_dag():
+    g, dag = RowsModel(page=16, pages=99, serving=1, greedy_loop=1, host_only=True).graph, M.compile_dag(2, [(0, 1)])
+    for name, args in (("tree_append", APPEND), ("tree_attend", ATTEND), ("tree_verify", VERIFY), ("tree_keep", KEEP)):
+        _refused(getattr(g, name), *args.values(), match="server")
+        _refused(getattr(dag, name), *args.values(), match="DAG")
+
+
+def test_constants():
+    text = open(M.binding.__file__.replace("paper_2512_22219_amd/binding.py", "include/mpk.h")).read()
+    assert "#define MPK_TREE_MAX_NODES 256u" in text and M.TREE_MAX_NODES == 256
+    assert "#define MPK_TREE_DRAWN_ONCE 1u" in text and M.TREE_DRAWN_ONCE == 1
