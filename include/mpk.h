@@ -708,7 +708,7 @@ mpk_status mpk_tree_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  * above -inf, the walk ends: next_tokens is -1, its logprob NaN.
  * Device errors: row_begin not ascending or outside 0 .. n_rows (lengths 0, next_tokens -1, nothing else is written); more nodes than
  * MPK_TREE_MAX_NODES, a parent that is no earlier node, a temperature that is negative or not finite (the sequence is
- * left out: its path is -1, its logprobs 0); a token outside 0 .. vocab - 1 that the walk comes to (never accepted). */
+ * left out: its path is -1, its logprobs 0); a token outside 0 .. vocab - 1 (never accepted). */
 #define MPK_TREE_DRAWN_ONCE 1u
 mpk_status mpk_tree_verify(mpk_graph *g, uint32_t n_seqs, uint32_t n_rows, const int32_t *row_begin,
                            const int32_t *parents, const int32_t *tokens, const void *logits, uint32_t logits_type,

@@ -59,6 +59,15 @@ struct LogprobArgs {
   uint32_t *err, *arrivals;
 };
 
+// What the workgroups of a sequence exchange (tree.hip): the graph's own memory, for what an earlier call left there must not pass for a
+// word of this one.
+constexpr uint32_t kVerifyChunks = 64, kVerifyDepth = 4;   // chunks of a row at most: a lane each when they are joined
+struct VerifySync {
+  uint32_t tag, left;   // of the last round of the last call; workgroups that have left this one
+  uint32_t pad[30];
+  uint64_t word[kVerifyDepth][4][kVerifyChunks];   // of a round and those before it
+};
+
 struct VerifyArgs {
   const int32_t* row_begin;   // [n_seqs + 1]
   const int32_t *parents, *tokens;   // [n_rows]
@@ -71,6 +80,8 @@ struct VerifyArgs {
   float* logprobs;   // or null
   void* work;
   uint32_t* err;
+  VerifySync* sync;   // [n_seqs]
+  bool jitter;        // delays at random (MPK_DEBUG_JITTER)
 };
 
 struct KeepArgs {

@@ -133,6 +133,7 @@ struct mpk_graph {
   // what the calls on rows (mpk_rows_*) need of the model
   uint16_t *cache_k = nullptr, *cache_v = nullptr;
   uint32_t* d_arrivals = nullptr;
+  VerifySync* d_verify = nullptr;   // [batch]
   std::vector<std::pair<const uint16_t*, const uint16_t*>> qk_gains;   // per layer: q_norm, k_norm (null without the norm)
 };
 
@@ -431,6 +432,7 @@ extern "C" mpk_status mpk_compile(const mpk_model_config* cfg, const mpk_weight_
   control.add(&g->d_counters, h.events.size());
   control.add(&g->d_err, 8);
   control.add(&g->d_arrivals, kRowsArrivals * kArrivalStride);
+  control.add(&g->d_verify, std::min(cfg->batch, kMaxRowSeqs));
   control.add(&g->d_grp, h.n_group_counters);
   control.add(&g->d_hier, (size_t)std::max(h.n_hier_events, 1u) * kHierWordsPerEvent);
   if (o.debug_flags & MPK_DEBUG_TRACE) control.add(&g->d_trace, h.tasks.size() * kTraceSlots);
@@ -741,6 +743,7 @@ extern "C" mpk_status mpk_graph_reset(mpk_graph* g) {
   HIP_TRY(hipMemset(g->d_counters, 0, g->h.events.size() * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_err, 0, 8 * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_arrivals, 0, kRowsArrivals * kArrivalStride * sizeof(uint32_t)));
+  HIP_TRY(hipMemset(g->d_verify, 0, std::min(g->h.cfg.batch, kMaxRowSeqs) * sizeof(VerifySync)));
   HIP_TRY(hipMemset(g->d_hier, 0, (size_t)std::max(g->h.n_hier_events, 1u) * kHierWordsPerEvent * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_grp, 0, std::max<size_t>(g->h.n_group_counters, 1) * sizeof(uint32_t)));
   HIP_TRY(hipMemset(g->d_rope, 0xFF, g->rope_words * sizeof(float)));
@@ -1158,6 +1161,7 @@ static mpk_status rows_words(const char* name, const void* p) {   // (NULL where
 }
 constexpr uint32_t kRowsMost = 1u << 24;   // rows of a call
 constexpr uint32_t kRowsMostSeq = 1u << 28;   // max_seq of the graph
+constexpr uint32_t kRowsMostVocab = 1u << 30;   // vocab of a graph whose trees are verified
 static mpk_status rows_count(uint32_t n_rows) {
   if (n_rows > kRowsMost) { set_error("n_rows %u is above %u", n_rows, kRowsMost); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
@@ -1313,6 +1317,7 @@ extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_
   const HostGraph& h = g->h;
   if (!h.cfg.vocab) { set_error("the graph is a task DAG, not a model"); return MPK_ERR_INVALID_ARG; }
   const uint32_t vocab = h.cfg.vocab;
+  if (vocab > kRowsMostVocab) { set_error("vocab %u is above %u", vocab, kRowsMostVocab); return MPK_ERR_UNSUPPORTED; }
   if (n_seqs == 0 || n_seqs > std::min(h.cfg.batch, kMaxRowSeqs)) { set_error("n_seqs %u is outside 1..%u, the graph's batch", n_seqs, h.cfg.batch); return MPK_ERR_INVALID_ARG; }
   if (logits_type > MPK_ROWS_F32) { set_error("unknown logits_type %u", logits_type); return MPK_ERR_INVALID_ARG; }
   if (flags & ~MPK_TREE_DRAWN_ONCE) { set_error("unknown flags bits"); return MPK_ERR_INVALID_ARG; }
@@ -1340,7 +1345,7 @@ extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_
   a.logits = logits; a.stride = row_stride; a.draft = draft_probs; a.draft_stride = draft_stride;
   a.temperatures = temperatures; a.uniforms = uniforms;
   a.lengths = lengths; a.path = path; a.next = next_tokens; a.logprobs = logprobs;
-  a.work = workspace; a.err = g->d_err;
+  a.work = workspace; a.err = g->d_err; a.sync = g->d_verify; a.jitter = g->h.opt.debug_flags & MPK_DEBUG_JITTER;
   HIP_TRY(launch_tree_verify(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
   return MPK_OK;
 }

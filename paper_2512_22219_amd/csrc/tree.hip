@@ -1,224 +1,614 @@
 // Trees of drafted tokens: which of them stay (mpk_tree_verify), and their rows in the cache closed up (mpk_tree_keep).
 #include <algorithm>
+#include <type_traits>
 
 #include "rows_device.h"
 
 namespace mpk {
 
 // ------------------------------------------------------------------------------------ verify
-constexpr uint32_t kVerifyThreads = 1024, kVerifyWaves = kVerifyThreads / 64;
+// The walk needs, of each node that it comes to, the largest logit m and Z = sum 2^(k (x - m)), k = log2(e) / temperature, in 64 bits: a random
+// number is compared with sums of up to a vocabulary of weights, and which side it falls on is a token.
+// It goes in rounds.  A round is a node of the walk or, with a draft distribution, what is left of the node's distribution behind a refused
+// child.  A row is cut into chunks, one for each of the sequence's workgroups.  Each leaves its sums where all of them read
+// them, reads all of them, and works out for itself how the walk goes on.
+// So a round is one pass over a chunk and one exchange between the compute units, and nobody waits for a decision to be passed on.
+// Nor does anybody depend on workgroups that may not run yet: sums that have not come after a while are worked out by
+// who needs them (the same operations in the same order, the same bits), so that each workgroup alone comes to the end.
+constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
+constexpr uint32_t kVerifyLane = 16, kVerifyStep = kVerifyThreads * kVerifyLane;   // logits of a thread and of a workgroup at once
+constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once
+constexpr uint32_t kVerifyPatience = 2000;   // ticks of 10 ns until others' sums are worked out
+
+
+struct VerifyPlan {
+  uint32_t chunks, steps;   // of a row: a workgroup each; of a chunk
+};
+// What became of a node's children: one of them was accepted (its place), or none (the walk ends), the row has no distribution, or the
+// next is to be tried on what is left behind one refused.
+enum : int32_t { kNone = -1, kNoDistribution = -2, kRefused = -3 };
+
+__device__ __forceinline__ void put64(uint64_t* p, uint64_t v) { __hip_atomic_store(as_global(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// 2^d for d <= 0, 0 below -1000 (and for -inf): a polynomial of degree 9 through the Chebyshev points of [-1/2, 1/2], within 1.9e-14 of the
+// value, and the power of two added to the exponent.
+template <bool ZERO = true>   // false: d is not below -1000
+__device__ __forceinline__ double exp2_64(double d) {
+  const double big = 6755399441055744.0;   // 1.5 x 2^52: the sum's low bits are d as a whole number
+  const double t = d + big, f = d - (t - big);
+  double p = 0x1.b6571de2f2351p-24;
+  p = fma(p, f, 0x1.63ef969a64d3cp-20);
+  p = fma(p, f, 0x1.ffcb76789860fp-17);
+  p = fma(p, f, 0x1.43088e257f341p-13);
+  p = fma(p, f, 0x1.5d87fe908f88ap-10);
+  p = fma(p, f, 0x1.3b2ab72b175eep-7);
+  p = fma(p, f, 0x1.c6b08d7044119p-5);
+  p = fma(p, f, 0x1.ebfbdff8149f2p-3);
+  p = fma(p, f, 0x1.62e42fefa39f7p-1);
+  p = fma(p, f, 0x1.000000000003dp+0);
+  const uint32_t hi = (uint32_t)__double2hiint(p) + ((uint32_t)__double2loint(t) << 20);
+  return ZERO && d < -1000. ? 0. : __hiloint2double((int)hi, __double2loint(p));
+}
+// (x and m as they are in 64 bits: their difference loses nothing that shows)
+__device__ __forceinline__ double weight(float x, double m, double k) { return exp2_64(((double)x - m) * k); }
+
+__device__ __forceinline__ double lane64(double v, uint32_t lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ double wave_sum64(double v) {
+  v += dpp64<0xB1>(v);    // lane ^ 1
+  v += dpp64<0x4E>(v);    // lane ^ 2
+  v += dpp64<0x141>(v);   // mirror of 8
+  v += dpp64<0x140>(v);   // mirror of 16
+  return (lane64(v, 0) + lane64(v, 16)) + (lane64(v, 32) + lane64(v, 48));
+}
+__device__ __forceinline__ double wave_before64(double v, double* all) {   // the sum over the lanes in front, and over all
+  const uint32_t row = (threadIdx.x & 63u) >> 4;
+  double x = v;
+  x += dpp64<0x111>(x);   // from 1, 2, 4 and 8 lanes in front, in a row of 16
+  x += dpp64<0x112>(x);
+  x += dpp64<0x114>(x);
+  x += dpp64<0x118>(x);
+  const double r0 = lane64(x, 15), r1 = r0 + lane64(x, 31), r2 = r1 + lane64(x, 47);
+  *all = r2 + lane64(x, 63);
+  return dpp64<0x111>(x) + (row == 0u ? 0. : row == 1u ? r0 : row == 2u ? r1 : r2);
+}
 
 template <typename T>
 __device__ __forceinline__ float logit_of(const T* p, size_t i) {
   if constexpr (sizeof(T) == 4) return as_global(p)[i];
   else return bf16_to_f32(as_global(p)[i]);
 }
-// The sum over the workgroup, in every thread, and in *before that over the threads in front.
-__device__ __forceinline__ double block_sum64(double v, double* red, double* before = nullptr) {
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  double in = v;
+// 16 bytes from an address of any alignment of the elements.
+typedef uint32_t u32x4_of4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_of2 __attribute__((ext_vector_type(4), aligned(2)));
+// N neighbouring elements of a row of n from the i-th on as fp32, `fill` behind the last; by loads of E of them, the row's last E where some of
+// these lie behind its end.
+template <uint32_t N, uint32_t E, typename T>
+__device__ __forceinline__ void load_row(const T* x, uint32_t i, uint32_t n, float fill, float* y) {
+  constexpr uint32_t PER = 16 / sizeof(T);
+  using Bytes = std::conditional_t<sizeof(T) == 4, u32x4_of4, u32x4_of2>;
+  if (n < E) {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const double x = __shfl_up(in, o, 64);
-    if (lane >= (uint32_t)o) in += x;
+    for (uint32_t j = 0; j < N; ++j) y[j] = j < E && i + j < n ? logit_of(x, i + j) : fill;
+    return;
   }
-  __syncthreads();
-  if (lane == 63u) red[wave] = in;
-  __syncthreads();
-  double all = 0., front = 0.;
-  for (uint32_t i = 0; i < kVerifyWaves; ++i) {
-    if (i == wave) front = all;
-    all += red[i];
+#pragma unroll
+  for (uint32_t j = 0; j < N; j += E) {
+    const uint32_t at = min(i + j, n - E);
+#pragma unroll
+    for (uint32_t l = 0; l < E; l += PER) {
+      const u32x4 b = *(const MPK_GLOBAL Bytes*)(x + at + l);
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        if constexpr (PER == 4) y[j + l + e] = __uint_as_float(b[e]);
+        else { y[j + l + 2 * e] = bf16_lo(b[e]); y[j + l + 2 * e + 1] = bf16_hi(b[e]); }
+      }
+    }
+    if (__any(at != i + j)) {   // (elements in front of the i-th have been read too: they are another load's)
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e) y[j + e] = at + e < i + j ? fill : y[j + e];
+    }
   }
-  if (before) *before = front + (in - v);
-  return all;
 }
+// Where the load of the i-th element (a multiple of E from a load's first) starts.
+__device__ __forceinline__ uint32_t row_start(uint32_t i, uint32_t n, uint32_t E) { return n < E ? i : min(i, n - E); }
 
-// The walk of one sequence from the root on.  p = softmax(row / temperature) in 64 bits: a random number is compared with sums
-// of up to a vocabulary of weights, and which side it falls on is a token.
-template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(VerifyArgs a) {
-  __shared__ double red[kVerifyWaves], scale[kTreeNodes], over[kTreeNodes];
-  __shared__ uint64_t best[kVerifyWaves];
-  __shared__ int32_t parent[kTreeNodes], gone[kTreeNodes];
-  __shared__ int32_t found[2];
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, seq = blockIdx.x;
+// T: the logits; DRAFT: there are draft distributions.
+template <typename T, bool DRAFT>
+__global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyArgs a, VerifyPlan p) {
+  constexpr uint32_t E = 16 / sizeof(T), V = kVerifyLane / E;   // logits of a load, loads of a step
+  __shared__ double part_sum[kVerifyChunks], total[kTreeNodes], over[kTreeNodes], scale[kTreeNodes], sums[kVerifyWaves];
+  __shared__ float part_max[kVerifyChunks], top[kTreeNodes], maxima[kVerifyWaves];
+  __shared__ uint32_t part_place[kVerifyChunks], places[kVerifyWaves], found[2], zeros[kVerifyThreads];
+  __shared__ struct { int32_t code; uint32_t lack, place, child, subtracted; } told;   // by wavefront 0
+  __shared__ uint8_t path[kTreeNodes];
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), seq = blockIdx.x % a.n_seqs, own = blockIdx.x / a.n_seqs;   // its chunk
+  VerifySync& sync = a.sync[seq];
+
+  // ---- the sequence, checked by every wavefront for itself
   int32_t b = 0, e = 0;
   if (lane < a.n_seqs) {
     b = as_global(a.row_begin)[lane];
     e = as_global(a.row_begin)[lane + 1];
   }
+  float temperature = 0.f;
+  if (a.temperatures) temperature = as_global(a.temperatures)[seq];
+  uint32_t tag = uniform_u32(ld_relaxed(&sync.tag));   // of the last round of the call before
+  const bool teller = own == 0u && wave == 0u;
   const uint64_t bad = __ballot(b < 0 || e < b || (uint32_t)e > a.n_rows);
   if (bad) {
-    if (seq == 0 && wave == 0 && lane == (uint32_t)__builtin_ctzll(bad)) report_rows(a.err, DE_BAD_ROWS, lane, (uint32_t)e);
+    if (teller && seq == 0 && lane == (uint32_t)__builtin_ctzll(bad)) report_rows(a.err, DE_BAD_ROWS, lane, (uint32_t)e);
     b = e = 0;
   }
   const uint32_t begin = (uint32_t)__builtin_amdgcn_readlane(b, seq), nodes = (uint32_t)__builtin_amdgcn_readlane(e, seq) - begin;
-  uint32_t length = 0;
-  int32_t next = -1;
   bool out = nodes == 0;
+  TreeLanes tree;
   if (nodes > kTreeNodes) {
-    if (threadIdx.x == 0) report_rows(a.err, DE_BAD_TREE, seq, nodes);
+    if (teller && lane == 0) report_rows(a.err, DE_BAD_TREE, seq, nodes);
     out = true;
-  }
-  float temperature = 0.f;
-  if (!out) {
-    TreeLanes tree;
+  } else if (!out) {
     uint32_t wrong = load_tree(a.parents + begin, nodes, &tree);
-    for (uint32_t t = 1; t < wrong; ++t)
-      if (parent_of(tree, t) < 0) wrong = t;   // (one root)
-    if (wrong < nodes) {
-      if (threadIdx.x == 0) report_rows(a.err, DE_BAD_PARENT, seq, wrong);
-      out = true;
-    }
-    if (threadIdx.x < nodes) parent[threadIdx.x] = as_global(a.parents)[begin + threadIdx.x];
-    if (a.temperatures) temperature = as_global(a.temperatures)[seq];
-    if (!(temperature >= 0.f && temperature < INFINITY)) {
-      if (threadIdx.x == 0) report_rows(a.err, DE_BAD_TEMPERATURE, seq, __float_as_uint(temperature));
-      out = true;
-    }
-    __syncthreads();
-  }
-  const bool greedy = temperature == 0.f;
-  const double inv_t = greedy ? 1. : 1. / (double)temperature;
-  uint32_t at = 0;
-  while (!out) {
-    const T* x = (const T*)a.logits + (size_t)(begin + at) * a.stride;
-    const float* q = a.draft && !greedy ? a.draft + (size_t)(begin + at) * a.draft_stride : nullptr;
-    if (threadIdx.x == 0) as_global(a.path)[begin + length] = (int32_t)at;
-    ++length;
-    // ---- the largest logit, of equal ones the first
-    uint64_t top = 0;
-    bool none = false;
-    for (uint32_t v = threadIdx.x; v < a.vocab; v += kVerifyThreads) {
-      const float y = logit_of(x, v);
-      none |= !(y < INFINITY);
-      const uint32_t u = __float_as_uint(y + 0.0f);
-      const uint64_t key = ((uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (0xFFFFFFFFu - v);
-      if (y > -INFINITY) top = max(top, key);
-    }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, o, 64));
-    __syncthreads();
-    if (lane == 0) best[wave] = top;
-    none = __syncthreads_or(none);
-    for (uint32_t i = 0; i < kVerifyWaves; ++i) top = max(top, best[i]);
-    if (none || !top) {   // no distribution
-      if (threadIdx.x == 0 && a.logprobs) as_global(a.logprobs)[begin + length - 1u] = __uint_as_float(0x7FC00000u);
-      break;
+    for (uint32_t i = kTreeNodes / 64u; i-- > 0;) {   // (one root)
+      const uint64_t roots = __ballot(tree.of[i] < 0 && 64u * i + lane < nodes) & ~(uint64_t)(i == 0u);
+      if (roots) wrong = min(wrong, 64u * i + (uint32_t)__builtin_ctzll(roots));
     }
-    const int32_t largest = (int32_t)(0xFFFFFFFFu - (uint32_t)top);
-    const double m = (double)logit_of(x, (size_t)largest);
-    double total = 0.;
-    if (!greedy || a.logprobs) {
-      double s = 0.;
-      for (uint32_t v = threadIdx.x; v < a.vocab; v += kVerifyThreads) s += exp(((double)logit_of(x, v) - m) * inv_t);
-      total = block_sum64(s, red);
-    }
-    // ---- its children in turn
-    uint32_t n_gone = 0;       // tokens that are ruled out (no draft distribution), or subtractions made (one)
-    double drawn = 0., mass = total;
-    // what is left of the row's distribution at v, not normed: mass is its sum
-    auto rest = [&](uint32_t v) {
-      double r = exp(((double)logit_of(x, v) - m) * inv_t);
-      if (q) {
-        const double qv = (double)as_global(q)[v];
-        for (uint32_t i = 0; i < n_gone; ++i) r = fmax(0., r * over[i] - scale[i] * qv);
-      } else {
-        for (uint32_t i = 0; i < n_gone; ++i) r = gone[i] == (int32_t)v ? 0. : r;
-      }
-      return r;
-    };
-    int32_t taken = -1;
-    for (uint32_t t = at + 1u; t < nodes && taken < 0; ++t) {
-      if (parent[t] != (int32_t)at) continue;
-      const int32_t token = as_global(a.tokens)[begin + t];
-      if (token < 0 || (uint32_t)token >= a.vocab) {
-        if (threadIdx.x == 0) report_rows(a.err, DE_BAD_TOKEN, seq, (uint32_t)token);
-        continue;
-      }
-      if (greedy) {
-        if (token == largest) taken = (int32_t)t;
-        continue;
-      }
-      const double u = (double)as_global(a.uniforms)[begin + t], r = rest((uint32_t)token);
-      if (!q) {
-        if (u * mass < r) { taken = (int32_t)t; continue; }
-        if (mass - r > 0.) {
-          mass -= r;
-          if (threadIdx.x == 0) gone[n_gone] = token;
-          ++n_gone;
+    if (wrong < nodes) {
+      if (teller && lane == 0) report_rows(a.err, DE_BAD_PARENT, seq, wrong);
+      out = true;
+    } else if (teller) {
+#pragma unroll
+      for (uint32_t i = 0; i < kTreeNodes / 64u; ++i) {
+        const uint32_t t = 64u * i + lane;
+        if (t > 0u && t < nodes) {
+          const int32_t token = as_global(a.tokens)[begin + t];
+          if (token < 0 || (uint32_t)token >= a.vocab) report_rows(a.err, DE_BAD_TOKEN, seq, (uint32_t)token);
         }
-        __syncthreads();
+      }
+    }
+    if (!(temperature >= 0.f && temperature < INFINITY)) {
+      if (teller && lane == 0) report_rows(a.err, DE_BAD_TEMPERATURE, seq, __float_as_uint(temperature));
+      out = true;
+    }
+  }
+  if (out) {
+    if (own) return;
+    if (threadIdx.x == 0) {
+      as_global(a.lengths)[seq] = 0;
+      as_global(a.next)[seq] = -1;
+    }
+    for (uint32_t t = threadIdx.x; t < nodes; t += kVerifyThreads) {
+      as_global(a.path)[begin + t] = -1;
+      if (a.logprobs) as_global(a.logprobs)[begin + t] = 0.f;
+    }
+    return;
+  }
+  const bool greedy = temperature == 0.f, weigh = !greedy || a.logprobs;
+  const double k = 1.4426950408889634 / (greedy ? 1. : (double)temperature);
+  const uint32_t chunk_logits = p.steps * kVerifyStep;
+  auto row_of = [&](uint32_t node) { return (const T*)a.logits + (size_t)(begin + node) * a.stride; };
+  auto draft_of = [&](uint32_t node) { return a.draft + (size_t)(begin + node) * a.draft_stride; };
+  auto parents_of = [&](uint32_t i) { return i == 0u ? tree.of[0] : i == 1u ? tree.of[1] : i == 2u ? tree.of[2] : tree.of[3]; };   // of the nodes 64 i + lane
+  auto token_of = [&](uint32_t t) {   // -1: none
+    const int32_t token = as_global(a.tokens)[begin + t];
+    return token < 0 || (uint32_t)token >= a.vocab ? -1 : token;
+  };
+
+  // ---- a chunk of a node's row, by the workgroup: a wavefront's largest logit, its first place, and the sum of the weights against that; then, in
+  // wavefront 0, the chunk's (in m a NaN: the row has no distribution).  The first step's logits may be there already.
+  auto request = [&](uint32_t node, uint32_t chunk, uint32_t step, float (&y)[kVerifyLane]) {
+    const T* x = row_of(node);
+    const uint32_t v0 = chunk * chunk_logits + step * kVerifyStep + threadIdx.x * E;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) load_row<E, E>(x, v0 + j * kVerifyThreads * E, a.vocab, -INFINITY, y + j * E);
+  };
+  auto sum_weights = [&](uint32_t node, uint32_t chunk, float (&y)[kVerifyLane], bool there, float& m, double& sum, uint32_t& first) {
+    float most = -INFINITY;
+    uint32_t at = 0xFFFFFFFFu;
+    double s = 0.;
+    bool none = false;
+    for (uint32_t step = 0; step < p.steps; ++step) {
+      if (step || !there) request(node, chunk, step, y);
+      float mx = y[0];
+#pragma unroll
+      for (uint32_t j = 0; j < kVerifyLane; ++j) {
+        mx = fmaxf(mx, y[j]);
+        none |= !(y[j] < INFINITY);
+      }
+      const float wm = wave_max_dpp(mx);
+      if (greedy && wm > most) {
+        uint32_t j = kVerifyLane;
+#pragma unroll
+        for (uint32_t l = kVerifyLane; l-- > 0;) j = y[l] == wm ? l : j;
+        at = j < kVerifyLane ? row_start(chunk * chunk_logits + step * kVerifyStep + (j / E * kVerifyThreads + threadIdx.x) * E, a.vocab, E) + j % E : 0xFFFFFFFFu;
+      }
+      if (wm > most) {
+        if (most > -INFINITY) s *= exp2_64(((double)most - (double)wm) * k);
+        most = wm;
+      }
+      if (weigh && most > -INFINITY) {
+        // (a weight below 2^-1000 is that here: neither shows in the sum)
+#pragma unroll
+        for (uint32_t j = 0; j < kVerifyLane; ++j) s += exp2_64<false>(fmax(((double)y[j] - (double)most) * k, -1000.));
+      }
+    }
+    s = wave_sum64(s);
+    if (greedy) at = wave_min_u32(at);
+    none = __any(none);
+    if (lane == 0) { maxima[wave] = none ? __uint_as_float(0x7FC00000u) : most; sums[wave] = s; places[wave] = at; }
+    __syncthreads();
+    if (wave) return;
+    m = maxima[0];
+    none = m != m;
+#pragma unroll
+    for (uint32_t i = 1; i < kVerifyWaves; ++i) { none |= maxima[i] != maxima[i]; m = fmaxf(m, maxima[i]); }
+    const float mine = maxima[lane % kVerifyWaves];   // (a lane each)
+    s = mine > -INFINITY ? sums[lane % kVerifyWaves] * weight(mine, (double)m, k) : 0.;
+    first = 0xFFFFFFFFu;
+    sum = 0.;
+#pragma unroll
+    for (uint32_t i = 0; i < kVerifyWaves; ++i) {
+      sum += lane64(s, i);
+      if (maxima[i] == m) first = min(first, places[i]);
+    }
+    if (none) m = __uint_as_float(0x7FC00000u);
+  };
+  // ... and what is left of it after n subtractions.
+  auto sum_rest = [&](uint32_t node, uint32_t chunk, uint32_t n, float (&y)[kVerifyLane], double& sum) {
+    const float* q = draft_of(node);
+    const uint32_t v0 = chunk * chunk_logits + threadIdx.x * E;
+    const double m = (double)top[node];
+    double s = 0.;
+    for (uint32_t step = 0; step < p.steps; ++step) {
+      float z[kVerifyLane];
+      request(node, chunk, step, y);
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) load_row<E, E>(q, v0 + step * kVerifyStep + j * kVerifyThreads * E, a.vocab, 0.f, z + j * E);
+#pragma unroll
+      for (uint32_t j = 0; j < kVerifyLane; ++j) {
+        double r = weight(y[j], m, k);
+        for (uint32_t i = 0; i < n; ++i) r = fmax(0., r * over[i] - (double)z[j] * scale[i]);
+        s += r;
+      }
+    }
+    s = wave_sum64(s);
+    if (lane == 0) sums[wave] = s;
+    __syncthreads();
+    if (wave == 0) sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  };
+
+  // ---- a wavefront: a node's children in turn.  Its lanes have the children among 64 nodes: token (-1: none), the token's logit, random number, draft.
+  struct Children {
+    int32_t token;
+    float x, u, q;
+  };
+  auto children_of = [&](uint32_t node, uint32_t i) {
+    const uint32_t t = 64u * i + lane;
+    Children c = {-1, 0.f, 0.f, 0.f};
+    if (t < nodes && parents_of(i) == (int32_t)node) c.token = token_of(t);
+    if (c.token >= 0 && !greedy) {
+      c.x = logit_of(row_of(node), (size_t)c.token);
+      c.u = as_global(a.uniforms)[begin + t];
+      if constexpr (DRAFT) c.q = as_global(draft_of(node))[c.token];
+    }
+    return c;
+  };
+  // Tokens that were chosen: r is w without the refused tokens, mass its sum; part is the sum of the lane's chunk, and loses them too.
+  // The first children are among the nodes that the node itself is among.
+  auto try_chosen = [&](uint32_t node, const Children& near, double m, uint32_t largest, double mass, double& part) -> int32_t {
+#pragma unroll 1
+    for (uint32_t i = node >> 6; i * 64u < nodes; ++i) {
+      const Children c = i == node >> 6 ? near : children_of(node, i);
+      if (greedy) {
+        const uint64_t same = __ballot(c.token >= 0 && (uint32_t)c.token == largest);
+        if (same) return (int32_t)(64u * i + (uint32_t)__builtin_ctzll(same));
         continue;
       }
-      if (a.flags & MPK_TREE_DRAWN_ONCE && drawn >= 1.) continue;   // (the distribution has no more tokens)
-      const double mine = (double)as_global(q)[token], norm = a.flags & MPK_TREE_DRAWN_ONCE ? 1. / (1. - drawn) : 1.;
-      if (u * norm * mine * mass < r) { taken = (int32_t)t; continue; }
-      drawn += mine;
-      __syncthreads();
-      if (threadIdx.x == 0) { over[n_gone] = 1. / mass; scale[n_gone] = norm; }
-      __syncthreads();
-      ++n_gone;
-      double s = 0.;
-      for (uint32_t v = threadIdx.x; v < a.vocab; v += kVerifyThreads) s += rest(v);
-      s = block_sum64(s, red);
-      if (s > 0.) mass = s;
-      else --n_gone;   // (nothing left: as it was)
+      const double w = c.token >= 0 ? weight(c.x, m, k) : 0.;
+      for (uint64_t set = __ballot(c.token >= 0); set; set &= set - 1ull) {
+        const uint32_t j = (uint32_t)__builtin_ctzll(set);
+        const int32_t mine = __builtin_amdgcn_readlane(c.token, j);
+        bool twin = lane < j && c.token == mine;   // of an earlier child: ruled out by now
+        for (uint32_t g = node >> 6; g < i; ++g) twin |= parents_of(g) == (int32_t)node && 64u * g + lane < nodes && token_of(64u * g + lane) == mine;
+        const double r = __any(twin) ? 0. : lane64(w, j), u = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c.u), j));
+        if (u * mass < r) return (int32_t)(64u * i + j);
+        if (mass - r > 0.) mass -= r;
+        if ((uint32_t)mine / chunk_logits == lane) part = fmax(0., part - r);
+      }
     }
-    if (taken >= 0) {
-      const int32_t token = as_global(a.tokens)[begin + taken];
-      if (threadIdx.x == 0 && a.logprobs) as_global(a.logprobs)[begin + length - 1u] = (float)(((double)logit_of(x, (size_t)token) - m) * inv_t - log(total));
-      at = (uint32_t)taken;
+    return kNone;
+  };
+  // Tokens that were drawn: r is w after n subtractions, mass its sum; the children from `child` on, until one is accepted or refused.  near:
+  // the children among the nodes that `child` is among.  norm: what a refused one's subtraction takes the draft times.
+  auto try_drawn = [&](uint32_t node, const Children& near, double m, double mass, uint32_t n, uint32_t& child, double& drawn, double& norm) -> int32_t {
+#pragma unroll 1
+    for (uint32_t i = child >> 6; i * 64u < nodes; ++i) {
+      const Children c = i == child >> 6 ? near : children_of(node, i);
+      const uint64_t set = __ballot(c.token >= 0 && 64u * i + lane >= child);
+      if (!set) continue;
+      if (a.flags & MPK_TREE_DRAWN_ONCE && drawn >= 1.) return kNone;   // (the distribution has no more tokens)
+      const uint32_t j = (uint32_t)__builtin_ctzll(set);
+      auto of_it = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j)); };
+      double r = weight(of_it(c.x), m, k);
+      const double share = (double)of_it(c.q), u = (double)of_it(c.u);
+      for (uint32_t s = 0; s < n; ++s) r = fmax(0., r * over[s] - share * scale[s]);
+      norm = a.flags & MPK_TREE_DRAWN_ONCE ? 1. / (1. - drawn) : 1.;
+      if (u * norm * share * mass < r) return (int32_t)(64u * i + j);
+      drawn += share;
+      child = 64u * i + j + 1u;
+      return kRefused;
+    }
+    return kNone;
+  };
+
+  // ---- the exchange: a chunk's sums in words that have the round's tag each (the place where something is greedy)
+  const uint32_t words = greedy ? 4u : 3u;
+  auto leave = [&](float m, double sum, uint32_t first) {
+    if (lane < words) {
+      const uint32_t v = lane == 0u ? __float_as_uint(m) : lane == 1u ? (uint32_t)__double2hiint(sum) : lane == 2u ? (uint32_t)__double2loint(sum) : first;
+      put64(&sync.word[tag % kVerifyDepth][lane][own], (uint64_t)tag << 32 | v);
+    }
+  };
+
+  // ---- rounds
+  uint32_t at = 0, length = 1, child = 0, subtracted = 0;   // the walk's node, its nodes; the children to be tried, from here on; the node's subtractions
+  int32_t ended;
+  const double uniform = greedy ? 0. : (double)as_global(a.uniforms)[begin];   // of the root: for the next token
+  if (threadIdx.x == 0) path[0] = 0;
+  float y[kVerifyLane];
+  uint32_t next_guess = kTreeNodes;   // whose, the node's first child
+  bool there = false, rest = false;   // the chunk's first logits are in y; the round is of what is left of the node's row
+  double now = 0., drawn = 0., mass = 0.;   // wavefront 0: the lane's chunk, the draft's share of the refused tokens, the sum of the chunks
+  for (;;) {
+    ++tag;
+    if (a.jitter) {   // (MPK_DEBUG_JITTER: up to twice the others' patience)
+      const uint64_t t0 = wall_clock64(), wait = (uint64_t)((tag * 2654435761u ^ blockIdx.x * 2246822519u) >> 16) % (2u * kVerifyPatience);
+      while (wall_clock64() - t0 < wait) __builtin_amdgcn_s_sleep(8);
+    }
+    // The children and their logits are on their way beside the chunk
+    Children near = {-1, 0.f, 0.f, 0.f};
+    if (wave == 0) near = children_of(at, child >> 6);
+    // ---- this workgroup's chunk, then the others' sums into part_max, part_sum and part_place
+    bool got = wave != 0 || lane >= p.chunks;
+    uint32_t chunk = own;
+    for (uint32_t patience = kVerifyPatience;; patience = 0) {
+      float m = 0.f;
+      double sum = 0.;
+      uint32_t first = 0;
+      if (DRAFT && rest) sum_rest(at, chunk, subtracted, y, sum);
+      else sum_weights(at, chunk, y, there && patience, m, sum, first);
+      there = false;
+      if (patience) {
+        if (wave == 0) leave(m, sum, first);
+        if (!rest) {
+          // The walk's next node is the first child more often than not: its chunk is on its way while the others' sums are
+          uint32_t guess = kTreeNodes;
+          for (uint32_t g = at >> 6; g * 64u < nodes && guess == kTreeNodes; ++g) {
+            const uint64_t set = __ballot(64u * g + lane < nodes && parents_of(g) == (int32_t)at);
+            if (set) guess = 64u * g + (uint32_t)__builtin_ctzll(set);
+          }
+          if (guess != kTreeNodes) {
+            request(guess, own, 0u, y);
+            there = true;
+          }
+          next_guess = guess;
+        }
+      } else if (wave == 0 && lane == chunk) {
+        part_max[lane] = m;
+        part_sum[lane] = sum;
+        part_place[lane] = first;
+        got = true;
+      }
+      if (wave == 0) {
+        uint64_t lacks, since = 0;
+        for (;;) {
+          bool ahead = false;   // (others are a round ahead: it will not come)
+          if (!got) {
+            uint64_t w[4];
+#pragma unroll
+            for (uint32_t l = 0; l < 4; ++l) w[l] = l < words ? ld_relaxed64(&sync.word[tag % kVerifyDepth][l][lane]) : (uint64_t)tag << 32;
+            got = true;
+#pragma unroll
+            for (uint32_t l = 0; l < 4; ++l) got &= (uint32_t)(w[l] >> 32) == tag;
+            ahead = (int32_t)((uint32_t)(w[0] >> 32) - tag) > 0;
+            if (got) {
+              part_max[lane] = __uint_as_float((uint32_t)w[0]);
+              part_sum[lane] = __hiloint2double((int)(uint32_t)w[1], (int)(uint32_t)w[2]);
+              part_place[lane] = (uint32_t)w[3];
+            }
+          }
+          lacks = __ballot(!got);
+          if (!lacks || __any(ahead)) break;
+          if (!since) since = wall_clock64();
+          else if (wall_clock64() - since > patience) break;
+        }
+        if (lacks) {
+          if (lane == 0) told.lack = (uint32_t)__builtin_ctzll(lacks);
+        } else {
+          // ---- the row's sums over its chunks, and the node's children
+          int32_t c = kNoDistribution;
+          double m;
+          if (!rest) {
+            const float mc = lane < p.chunks ? part_max[lane] : -INFINITY, most = wave_max_dpp(mc);
+            const bool none = __any(mc != mc) || most == -INFINITY;
+            m = (double)most;
+            now = mc > -INFINITY ? part_sum[lane] * weight(mc, m, k) : 0.;
+            mass = wave_sum64(now);
+            drawn = 0.;
+            const uint32_t largest = greedy ? wave_min_u32(mc == most && lane < p.chunks ? part_place[lane] : 0xFFFFFFFFu) : 0u;
+            if (lane == 0) {
+              top[at] = most;
+              total[at] = mass;
+              told.place = largest;
+            }
+            if (!none) c = !DRAFT || greedy ? try_chosen(at, near, m, largest, mass, now) : kRefused;
+          } else {
+            m = (double)top[at];
+            const double part = lane < p.chunks ? part_sum[lane] : 0., s = wave_sum64(part);
+            if (s > 0.) { mass = s; now = part; }
+            else --subtracted;   // (nothing would be left: as it was)
+            c = kRefused;
+          }
+          if (DRAFT && c == kRefused) {
+            double norm;
+            c = try_drawn(at, near, m, mass, subtracted, child, drawn, norm);
+            if (lane == 0) {
+              if (c == kRefused) { over[subtracted] = 1. / mass; scale[subtracted] = norm; }
+              told.child = child;
+              told.subtracted = subtracted;
+            }
+          }
+          if (lane == 0) { told.code = c; told.lack = kVerifyChunks; }
+        }
+      }
       __syncthreads();
+      chunk = uniform_u32(told.lack);
+      if (chunk == kVerifyChunks) break;   // (else one that is not there after a while: worked out here)
+      __syncthreads();
+    }
+    // ---- the walk
+    ended = (int32_t)uniform_u32((uint32_t)told.code);
+    if (DRAFT) {
+      child = uniform_u32(told.child);
+      subtracted = uniform_u32(told.subtracted);
+    }
+    rest = DRAFT && ended == kRefused;
+    if (rest) {
+      ++subtracted;
+      there = false;
       continue;
     }
-    // ---- the end of the walk: the token that follows
-    if (greedy) next = largest;
-    else {
-      const uint32_t share = (a.vocab + kVerifyThreads - 1u) / kVerifyThreads, v0 = min(a.vocab, threadIdx.x * share), v1 = min(a.vocab, v0 + share);
-      double s = 0.;
-      for (uint32_t v = v0; v < v1; ++v) s += rest(v);
-      double before;
-      const double all = block_sum64(s, red, &before), goal = (double)as_global(a.uniforms)[begin] * all;
-      // the first thread whose end is beyond the goal; by rounding there may be none: the last that has anything
-      const uint64_t beyond = __ballot(s > 0. && before + s > goal), any = __ballot(s > 0.);
-      if (threadIdx.x == 0) { found[0] = 0x7FFFFFFF; found[1] = -1; }
-      __syncthreads();
-      if (lane == 0 && beyond) atomicMin(&found[0], (int32_t)(64u * wave + (uint32_t)__builtin_ctzll(beyond)));
-      if (lane == 0 && any) atomicMax(&found[1], (int32_t)(64u * wave + 63u - (uint32_t)__builtin_clzll(any)));
-      __syncthreads();
-      const int32_t who = found[0] != 0x7FFFFFFF ? found[0] : found[1];
-      __syncthreads();
-      if ((int32_t)threadIdx.x == who) {
-        double c = before;
-        for (uint32_t v = v0; v < v1; ++v) {
-          const double r = rest(v);
-          if (r > 0.) next = (int32_t)v;
-          c += r;
-          if (r > 0. && c > goal) break;
+    if (ended < 0) break;
+    there = there && (uint32_t)ended == next_guess;
+    at = (uint32_t)ended;
+    child = at & ~63u;
+    subtracted = 0;
+    if (threadIdx.x == 0) path[length] = (uint8_t)at;
+    ++length;
+  }
+  if (wave == 0) part_sum[lane] = now;
+  __syncthreads();
+
+  // ---- the end of the walk: the token that follows is drawn from what is left of the last node's row, in the first chunk that ends beyond
+  // the goal (by rounding there may be none: the last that has anything).  The workgroup that has this chunk writes the results.
+  const bool draws = ended == kNone && !greedy;
+  uint32_t chunk = 0;
+  double goal = 0.;
+  auto choose = [&]() {
+    double all;
+    const double mine = part_sum[lane], before = wave_before64(mine, &all);
+    const uint64_t any = __ballot(mine > 0.), beyond = __ballot(mine > 0. && before + mine > uniform * all);
+    chunk = beyond ? (uint32_t)__builtin_ctzll(beyond) : any ? 63u - (uint32_t)__builtin_clzll(any) : kVerifyChunks;
+    goal = uniform * all - lane64(before, chunk & 63u);
+  };
+  if (draws) choose();
+  if (own == (chunk == kVerifyChunks ? 0u : chunk)) {
+    // (what the path's nodes say about the tokens behind them, a thread each: on its way meanwhile)
+    float said = 0.f;
+    const uint32_t here = threadIdx.x < length ? path[threadIdx.x] : 0u;
+    if (a.logprobs && threadIdx.x + 1u < length) said = logit_of(row_of(here), (size_t)as_global(a.tokens)[begin + path[threadIdx.x + 1u]]);
+    int32_t token = ended == kNone && greedy ? (int32_t)told.place : -1;
+    if (draws) {
+      int32_t gone = -1;   // a child's token of the node: refused, as all of them are
+      if (!DRAFT && threadIdx.x < nodes && threadIdx.x > at && as_global(a.parents)[begin + threadIdx.x] == (int32_t)at) gone = token_of(threadIdx.x);
+      for (; chunk != kVerifyChunks; choose()) {
+        if (threadIdx.x == 0) { found[0] = 0xFFFFFFFFu; found[1] = 0; }
+        double front = 0.;
+        for (uint32_t step = 0; step < p.steps; ++step) {
+          const uint32_t v0 = chunk * chunk_logits + step * kVerifyStep, v = v0 + threadIdx.x * kVerifyLane;
+          float z[kVerifyLane];
+          load_row<kVerifyLane, E>(row_of(at), v, a.vocab, -INFINITY, y);
+          if (DRAFT && subtracted) load_row<kVerifyLane, E>(draft_of(at), v, a.vocab, 0.f, z);
+          if (!DRAFT) {
+            zeros[threadIdx.x] = 0;
+            __syncthreads();
+            const uint32_t o = ((uint32_t)gone - v0) / E * E;   // its load
+            if (gone >= 0 && (uint32_t)gone >= v0 && o < kVerifyStep) atomicOr(&zeros[o / kVerifyLane], 1u << (o % kVerifyLane + (uint32_t)gone - row_start(v0 + o, a.vocab, E)));
+            __syncthreads();
+          }
+          const uint32_t zero = DRAFT ? 0u : zeros[threadIdx.x];
+          double r[kVerifyLane], s = 0.;
+          const double m = (double)top[at];
+#pragma unroll
+          for (uint32_t j = 0; j < kVerifyLane; ++j) {
+            r[j] = weight(y[j], m, k);
+            if constexpr (DRAFT) {
+              for (uint32_t i = 0; i < subtracted; ++i) r[j] = fmax(0., r[j] * over[i] - (double)z[j] * scale[i]);
+            } else r[j] = zero >> j & 1u ? 0. : r[j];
+            s += r[j];
+          }
+          double all, before = wave_before64(s, &all);
+          if (lane == 0) sums[wave] = all;
+          __syncthreads();
+          before += front;
+#pragma unroll
+          for (uint32_t i = 0; i < kVerifyWaves; ++i) {
+            if (i < wave) before += sums[i];
+            front += sums[i];
+          }
+          const bool crosses = s > 0. && before + s > goal;
+          const uint64_t any = __ballot(s > 0.), cross = __ballot(crosses);
+          // the wavefront's first thread that ends beyond the goal, or its last that has anything
+          if (any && lane == (cross ? (uint32_t)__builtin_ctzll(cross) : 63u - (uint32_t)__builtin_clzll(any))) {
+            uint32_t last = 0, hit = 0xFFFFFFFFu;
+            double sum = before;
+#pragma unroll
+            for (uint32_t j = 0; j < kVerifyLane; ++j) {
+              sum += r[j];
+              const uint32_t place_j = row_start(v + j / E * E, a.vocab, E) + j % E;
+              last = r[j] > 0. ? place_j : last;
+              hit = r[j] > 0. && sum > goal && hit == 0xFFFFFFFFu ? place_j : hit;
+            }
+            if (crosses) atomicMin(&found[0], min(hit, last));
+            atomicMax(&found[1], last + 1u);
+          }
+          __syncthreads();
+          if (found[0] != 0xFFFFFFFFu) break;
         }
-        found[0] = next;
+        token = found[0] != 0xFFFFFFFFu ? (int32_t)found[0] : (int32_t)found[1] - 1;
+        if (token >= 0) break;
+        if (threadIdx.x == 0) part_sum[chunk] = 0.;   // (a sum that was rounding alone)
+        __syncthreads();
       }
-      __syncthreads();
-      next = found[0];
     }
-    if (threadIdx.x == 0 && a.logprobs) as_global(a.logprobs)[begin + length - 1u] = (float)(((double)logit_of(x, (size_t)next) - m) * inv_t - log(total));
-    break;
+    if (threadIdx.x == 0) {
+      as_global(a.lengths)[seq] = (int32_t)length;
+      as_global(a.next)[seq] = token;
+    }
+    if (a.logprobs && threadIdx.x + 1u == length && token >= 0) said = logit_of(row_of(at), (size_t)token);
+    if (threadIdx.x < nodes) {
+      const uint32_t t = threadIdx.x;
+      as_global(a.path)[begin + t] = t < length ? (int32_t)here : -1;
+      if (a.logprobs) {
+        float lp = 0.f;
+        if (t < length) {
+          lp = (float)(((double)said - (double)top[here]) * k * 0.69314718055994531 - log(total[here]));
+          if (t + 1u == length && token < 0) lp = __uint_as_float(0x7FC00000u);
+        }
+        as_global(a.logprobs)[begin + t] = lp;
+      }
+    }
   }
-  if (threadIdx.x == 0) {
-    as_global(a.lengths)[seq] = (int32_t)length;
-    as_global(a.next)[seq] = next;
-  }
-  for (uint32_t t = length + threadIdx.x; t < nodes; t += kVerifyThreads) {
-    as_global(a.path)[begin + t] = -1;
-    if (a.logprobs) as_global(a.logprobs)[begin + t] = 0.f;
+  // ---- who leaves last leaves the tag for the next call
+  if (threadIdx.x == 0 && __hip_atomic_fetch_add(as_global(&sync.left), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == p.chunks) {
+    st_act_u32(&sync.left, 0u);
+    st_act_u32(&sync.tag, tag);
   }
 }
 
 hipError_t launch_tree_verify(const VerifyArgs& a, bool f32, hipStream_t stream) {
-  if (f32) tree_verify_kernel<float><<<dim3(a.n_seqs), dim3(kVerifyThreads), 0, stream>>>(a);
-  else tree_verify_kernel<uint16_t><<<dim3(a.n_seqs), dim3(kVerifyThreads), 0, stream>>>(a);
+  VerifyPlan p{};
+  const uint32_t most = std::min(kVerifyChunks, kVerifyWorkgroups / a.n_seqs);
+  p.steps = (a.vocab + most * kVerifyStep - 1u) / (most * kVerifyStep);
+  p.chunks = (a.vocab + p.steps * kVerifyStep - 1u) / (p.steps * kVerifyStep);
+  auto run = [&](auto kernel) { kernel<<<dim3(p.chunks * a.n_seqs), dim3(kVerifyThreads), 0, stream>>>(a, p); };
+  if (a.draft) run(f32 ? tree_verify_kernel<float, true> : tree_verify_kernel<uint16_t, true>);
+  else run(f32 ? tree_verify_kernel<float, false> : tree_verify_kernel<uint16_t, false>);
   return hipGetLastError();
 }
 

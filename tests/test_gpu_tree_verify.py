@@ -60,9 +60,9 @@ def _check(m, begin, parents, tokens, logits, out, temperatures, uniforms, draft
     assert (path[~mine] == 77).all() and (lp[~mine] == 77).all()
 
 
-def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperatures=None, first=0, behind=0, pad=0, std=2.0, batch=16, masked=0.0):
+def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperatures=None, first=0, behind=0, pad=0, std=2.0, batch=16, masked=0.0, **opts):
     gen = torch.Generator().manual_seed(seed)
-    m = TreeModel(n_q=2, n_kv=1, batch=batch, max_seq=8, vocab=vocab, layers=1)
+    m = TreeModel(n_q=2, n_kv=1, batch=batch, max_seq=8, vocab=vocab, layers=1, **opts)
     begin = _begin(lens, first)
     rows = begin[-1] + behind
     parents = [55] * first + sum((tree(n, k, seed + i) for i, (n, k) in enumerate(zip(lens, kinds))), []) + [-55] * behind
@@ -109,6 +109,14 @@ def test_verify(vocab, pad, draft, dtype):
 @pytest.mark.parametrize("temperatures", [None, [0.0], [1.0], [0.25, 4.0]])
 def test_verify_at_a_large_vocabulary(draft, temperatures):
     _case(3, 151936, [8, 1, 5], ["random", "chain", "star"], torch.bfloat16, draft, temperatures)
+
+
+@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("draft", [None, "drawn", "once"])
+def test_workgroups_that_are_late(draft, seed):
+    """Every workgroup waits at random, in each round, up to twice as long as the others wait for it: the same tokens."""
+    for dtype in (torch.float32, torch.bfloat16):
+        _case(seed, 70001, [9, 1, 30], ["chain", "chain", "random"], dtype, draft, [1.0, 0.0, 0.8], debug_flags=M.DEBUG_JITTER)
 
 
 @pytest.mark.parametrize("draft", [None, "once"])
