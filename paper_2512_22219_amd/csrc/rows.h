@@ -61,11 +61,11 @@ struct LogprobArgs {
 
 // What the workgroups of a sequence exchange (tree.hip): the graph's own memory, for what an earlier call left there must not pass for a
 // word of this one.
-constexpr uint32_t kVerifyChunks = 64, kVerifyDepth = 4;   // chunks of a row at most: a lane each when they are joined
+constexpr uint32_t kVerifyChunks = 128, kVerifyDepth = 4;   // chunks of a row at most
 struct VerifySync {
   uint32_t tag, left;   // of the last round of the last call; workgroups that have left this one
   uint32_t pad[30];
-  uint64_t word[kVerifyDepth][4][kVerifyChunks];   // of a round and those before it
+  uint64_t word[kVerifyDepth][kVerifyChunks][8];   // of a round and those before it
 };
 
 struct VerifyArgs {

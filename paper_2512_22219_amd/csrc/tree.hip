@@ -16,7 +16,8 @@ namespace mpk {
 // Nor does anybody depend on workgroups that may not run yet: sums that have not come after a while are worked out by
 // who needs them (the same operations in the same order, the same bits), so that each workgroup alone comes to the end.
 constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
-constexpr uint32_t kVerifyLane = 16, kVerifyStep = kVerifyThreads * kVerifyLane;   // logits of a thread and of a workgroup at once
+constexpr uint32_t kVerifyLane = 8, kVerifyStep = kVerifyThreads * kVerifyLane;   // logits of a thread and of a workgroup at once
+constexpr uint32_t kVerifyEach = kVerifyChunks / 64;   // chunks of a lane when they are joined: the lane-th, the 64 + lane-th
 constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once
 constexpr uint32_t kVerifyPatience = 2000;   // ticks of 10 ns until others' sums are worked out
 
@@ -123,8 +124,8 @@ template <typename T, bool DRAFT>
 __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyArgs a, VerifyPlan p) {
   constexpr uint32_t E = 16 / sizeof(T), V = kVerifyLane / E;   // logits of a load, loads of a step
   __shared__ double part_sum[kVerifyChunks], total[kTreeNodes], over[kTreeNodes], scale[kTreeNodes], sums[kVerifyWaves];
-  __shared__ float part_max[kVerifyChunks], top[kTreeNodes], maxima[kVerifyWaves];
-  __shared__ uint32_t part_place[kVerifyChunks], places[kVerifyWaves], found[2], zeros[kVerifyThreads];
+  __shared__ float top[kTreeNodes], maxima[kVerifyWaves], hit_logit[kVerifyWaves];
+  __shared__ uint32_t places[kVerifyWaves], hit[kVerifyWaves], last[kVerifyWaves], zeros[kVerifyThreads];
   __shared__ struct { int32_t code; uint32_t lack, place, child, subtracted; } told;   // by wavefront 0
   __shared__ uint8_t path[kTreeNodes];
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), seq = blockIdx.x % a.n_seqs, own = blockIdx.x / a.n_seqs;   // its chunk
@@ -147,6 +148,16 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   }
   const uint32_t begin = (uint32_t)__builtin_amdgcn_readlane(b, seq), nodes = (uint32_t)__builtin_amdgcn_readlane(e, seq) - begin;
   bool out = nodes == 0;
+  float y[kVerifyLane];   // a chunk's first logits: the root's are on their way meanwhile
+  auto row_of = [&](uint32_t node) { return (const T*)a.logits + (size_t)(begin + node) * a.stride; };
+  const uint32_t chunk_logits = p.steps * kVerifyStep;
+  auto request = [&](uint32_t node, uint32_t chunk, uint32_t step, float (&y)[kVerifyLane]) {
+    const T* x = row_of(node);
+    const uint32_t v0 = chunk * chunk_logits + step * kVerifyStep + threadIdx.x * E;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) load_row<E, E>(x, v0 + j * kVerifyThreads * E, a.vocab, -INFINITY, y + j * E);
+  };
+  if (!out) request(0u, own, 0u, y);
   TreeLanes tree;
   if (nodes > kTreeNodes) {
     if (teller && lane == 0) report_rows(a.err, DE_BAD_TREE, seq, nodes);
@@ -190,8 +201,6 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   }
   const bool greedy = temperature == 0.f, weigh = !greedy || a.logprobs;
   const double k = 1.4426950408889634 / (greedy ? 1. : (double)temperature);
-  const uint32_t chunk_logits = p.steps * kVerifyStep;
-  auto row_of = [&](uint32_t node) { return (const T*)a.logits + (size_t)(begin + node) * a.stride; };
   auto draft_of = [&](uint32_t node) { return a.draft + (size_t)(begin + node) * a.draft_stride; };
   auto parents_of = [&](uint32_t i) { return i == 0u ? tree.of[0] : i == 1u ? tree.of[1] : i == 2u ? tree.of[2] : tree.of[3]; };   // of the nodes 64 i + lane
   auto token_of = [&](uint32_t t) {   // -1: none
@@ -201,19 +210,17 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
 
   // ---- a chunk of a node's row, by the workgroup: a wavefront's largest logit, its first place, and the sum of the weights against that; then, in
   // wavefront 0, the chunk's (in m a NaN: the row has no distribution).  The first step's logits may be there already.
-  auto request = [&](uint32_t node, uint32_t chunk, uint32_t step, float (&y)[kVerifyLane]) {
-    const T* x = row_of(node);
-    const uint32_t v0 = chunk * chunk_logits + step * kVerifyStep + threadIdx.x * E;
-#pragma unroll
-    for (uint32_t j = 0; j < V; ++j) load_row<E, E>(x, v0 + j * kVerifyThreads * E, a.vocab, -INFINITY, y + j * E);
-  };
-  auto sum_weights = [&](uint32_t node, uint32_t chunk, float (&y)[kVerifyLane], bool there, float& m, double& sum, uint32_t& first) {
+  auto sum_weights = [&](uint32_t node, uint32_t chunk, float (&ahead)[kVerifyLane], bool there, float& m, double& sum, uint32_t& first) {
     float most = -INFINITY;
     uint32_t at = 0xFFFFFFFFu;
     double s = 0.;
     bool none = false;
+    if (!there) request(node, chunk, 0u, ahead);
     for (uint32_t step = 0; step < p.steps; ++step) {
-      if (step || !there) request(node, chunk, step, y);
+      float y[kVerifyLane];
+#pragma unroll
+      for (uint32_t j = 0; j < kVerifyLane; ++j) y[j] = ahead[j];
+      if (step + 1u < p.steps) request(node, chunk, step + 1u, ahead);
       float mx = y[0];
 #pragma unroll
       for (uint32_t j = 0; j < kVerifyLane; ++j) {
@@ -259,22 +266,33 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     if (none) m = __uint_as_float(0x7FC00000u);
   };
   // ... and what is left of it after n subtractions.
-  auto sum_rest = [&](uint32_t node, uint32_t chunk, uint32_t n, float (&y)[kVerifyLane], double& sum) {
+  auto sum_rest = [&](uint32_t node, uint32_t chunk, uint32_t n, float (&ahead)[kVerifyLane], double& sum) {
     const float* q = draft_of(node);
     const uint32_t v0 = chunk * chunk_logits + threadIdx.x * E;
     const double m = (double)top[node];
     double s = 0.;
+    float z_ahead[kVerifyLane];
+    auto request_both = [&](uint32_t step) {
+      request(node, chunk, step, ahead);
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) load_row<E, E>(q, v0 + step * kVerifyStep + j * kVerifyThreads * E, a.vocab, 0.f, z_ahead + j * E);
+    };
+    request_both(0u);
     for (uint32_t step = 0; step < p.steps; ++step) {
-      float z[kVerifyLane];
-      request(node, chunk, step, y);
+      float y[kVerifyLane], z[kVerifyLane];
 #pragma unroll
-      for (uint32_t j = 0; j < V; ++j) load_row<E, E>(q, v0 + step * kVerifyStep + j * kVerifyThreads * E, a.vocab, 0.f, z + j * E);
+      for (uint32_t j = 0; j < kVerifyLane; ++j) { y[j] = ahead[j]; z[j] = z_ahead[j]; }
+      if (step + 1u < p.steps) request_both(step + 1u);
+      double r[kVerifyLane];
 #pragma unroll
-      for (uint32_t j = 0; j < kVerifyLane; ++j) {
-        double r = weight(y[j], m, k);
-        for (uint32_t i = 0; i < n; ++i) r = fmax(0., r * over[i] - (double)z[j] * scale[i]);
-        s += r;
+      for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = weight(y[j], m, k);
+      for (uint32_t i = 0; i < n; ++i) {
+        const double o = over[i], f = scale[i];
+#pragma unroll
+        for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = fmax(0., r[j] * o - (double)z[j] * f);
       }
+#pragma unroll
+      for (uint32_t j = 0; j < kVerifyLane; ++j) s += r[j];
     }
     s = wave_sum64(s);
     if (lane == 0) sums[wave] = s;
@@ -298,9 +316,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     }
     return c;
   };
-  // Tokens that were chosen: r is w without the refused tokens, mass its sum; part is the sum of the lane's chunk, and loses them too.
+  // Tokens that were chosen: r is w without the refused tokens, mass its sum; part are the sums of the lane's chunks, and lose them too.
   // The first children are among the nodes that the node itself is among.
-  auto try_chosen = [&](uint32_t node, const Children& near, double m, uint32_t largest, double mass, double& part) -> int32_t {
+  auto try_chosen = [&](uint32_t node, const Children& near, double m, uint32_t largest, double mass, double (&part)[kVerifyEach]) -> int32_t {
 #pragma unroll 1
     for (uint32_t i = node >> 6; i * 64u < nodes; ++i) {
       const Children c = i == node >> 6 ? near : children_of(node, i);
@@ -318,7 +336,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
         const double r = __any(twin) ? 0. : lane64(w, j), u = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c.u), j));
         if (u * mass < r) return (int32_t)(64u * i + j);
         if (mass - r > 0.) mass -= r;
-        if ((uint32_t)mine / chunk_logits == lane) part = fmax(0., part - r);
+        const uint32_t of = (uint32_t)mine / chunk_logits;
+#pragma unroll
+        for (uint32_t h = 0; h < kVerifyEach; ++h) part[h] = of == 64u * h + lane ? fmax(0., part[h] - r) : part[h];
       }
     }
     return kNone;
@@ -351,7 +371,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   auto leave = [&](float m, double sum, uint32_t first) {
     if (lane < words) {
       const uint32_t v = lane == 0u ? __float_as_uint(m) : lane == 1u ? (uint32_t)__double2hiint(sum) : lane == 2u ? (uint32_t)__double2loint(sum) : first;
-      put64(&sync.word[tag % kVerifyDepth][lane][own], (uint64_t)tag << 32 | v);
+      put64(&sync.word[tag % kVerifyDepth][own][lane], (uint64_t)tag << 32 | v);
     }
   };
 
@@ -360,10 +380,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   int32_t ended;
   const double uniform = greedy ? 0. : (double)as_global(a.uniforms)[begin];   // of the root: for the next token
   if (threadIdx.x == 0) path[0] = 0;
-  float y[kVerifyLane];
-  uint32_t next_guess = kTreeNodes;   // whose, the node's first child
-  bool there = false, rest = false;   // the chunk's first logits are in y; the round is of what is left of the node's row
-  double now = 0., drawn = 0., mass = 0.;   // wavefront 0: the lane's chunk, the draft's share of the refused tokens, the sum of the chunks
+  bool there = true, rest = false;   // the chunk's first logits are on their way; the round is of what is left of the node's row
+  double now[kVerifyEach] = {}, drawn = 0., mass = 0.;   // wavefront 0: the lane's chunks, the draft's share of the refused tokens, the sum of the chunks
   for (;;) {
     ++tag;
     if (a.jitter) {   // (MPK_DEBUG_JITTER: up to twice the others' patience)
@@ -373,9 +391,18 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     // The children and their logits are on their way beside the chunk
     Children near = {-1, 0.f, 0.f, 0.f};
     if (wave == 0) near = children_of(at, child >> 6);
-    // ---- this workgroup's chunk, then the others' sums into part_max, part_sum and part_place
-    bool got = wave != 0 || lane >= p.chunks;
-    uint32_t chunk = own;
+    // ---- this workgroup's chunk, then the others' sums: wavefront 0 gets them
+    float part_max[kVerifyEach];
+    double part[kVerifyEach];
+    uint32_t part_place[kVerifyEach], chunk = own;
+    bool got[kVerifyEach];
+#pragma unroll
+    for (uint32_t h = 0; h < kVerifyEach; ++h) {
+      got[h] = 64u * h + lane >= p.chunks;
+      part_max[h] = -INFINITY;
+      part[h] = 0.;
+      part_place[h] = 0xFFFFFFFFu;
+    }
     for (uint32_t patience = kVerifyPatience;; patience = 0) {
       float m = 0.f;
       double sum = 0.;
@@ -385,73 +412,82 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       there = false;
       if (patience) {
         if (wave == 0) leave(m, sum, first);
-        if (!rest) {
-          // The walk's next node is the first child more often than not: its chunk is on its way while the others' sums are
-          uint32_t guess = kTreeNodes;
-          for (uint32_t g = at >> 6; g * 64u < nodes && guess == kTreeNodes; ++g) {
-            const uint64_t set = __ballot(64u * g + lane < nodes && parents_of(g) == (int32_t)at);
-            if (set) guess = 64u * g + (uint32_t)__builtin_ctzll(set);
-          }
-          if (guess != kTreeNodes) {
-            request(guess, own, 0u, y);
-            there = true;
-          }
-          next_guess = guess;
-        }
-      } else if (wave == 0 && lane == chunk) {
-        part_max[lane] = m;
-        part_sum[lane] = sum;
-        part_place[lane] = first;
-        got = true;
+      } else {
+#pragma unroll
+        for (uint32_t h = 0; h < kVerifyEach; ++h)
+          if (64u * h + lane == chunk) { part_max[h] = m; part[h] = sum; part_place[h] = first; got[h] = true; }
       }
       if (wave == 0) {
-        uint64_t lacks, since = 0;
+        uint64_t since = 0;
+        uint32_t lack;
         for (;;) {
           bool ahead = false;   // (others are a round ahead: it will not come)
-          if (!got) {
-            uint64_t w[4];
+          uint64_t w[kVerifyEach][4];
 #pragma unroll
-            for (uint32_t l = 0; l < 4; ++l) w[l] = l < words ? ld_relaxed64(&sync.word[tag % kVerifyDepth][l][lane]) : (uint64_t)tag << 32;
-            got = true;
+          for (uint32_t h = 0; h < kVerifyEach; ++h)
+            if (!got[h]) {
 #pragma unroll
-            for (uint32_t l = 0; l < 4; ++l) got &= (uint32_t)(w[l] >> 32) == tag;
-            ahead = (int32_t)((uint32_t)(w[0] >> 32) - tag) > 0;
-            if (got) {
-              part_max[lane] = __uint_as_float((uint32_t)w[0]);
-              part_sum[lane] = __hiloint2double((int)(uint32_t)w[1], (int)(uint32_t)w[2]);
-              part_place[lane] = (uint32_t)w[3];
+              for (uint32_t l = 0; l < 4; ++l) w[h][l] = l < words ? ld_relaxed64(&sync.word[tag % kVerifyDepth][64u * h + lane][l]) : (uint64_t)tag << 32;
             }
+          lack = kVerifyChunks;
+#pragma unroll
+          for (uint32_t h = kVerifyEach; h-- > 0;) {
+            if (!got[h]) {
+              got[h] = true;
+#pragma unroll
+              for (uint32_t l = 0; l < 4; ++l) got[h] &= (uint32_t)(w[h][l] >> 32) == tag;
+              ahead |= (int32_t)((uint32_t)(w[h][0] >> 32) - tag) > 0;
+              part_max[h] = __uint_as_float((uint32_t)w[h][0]);
+              part[h] = __hiloint2double((int)(uint32_t)w[h][1], (int)(uint32_t)w[h][2]);
+              part_place[h] = (uint32_t)w[h][3];
+            }
+            const uint64_t lacks = __ballot(!got[h]);
+            if (lacks) lack = 64u * h + (uint32_t)__builtin_ctzll(lacks);
           }
-          lacks = __ballot(!got);
-          if (!lacks || __any(ahead)) break;
+          if (lack == kVerifyChunks || __any(ahead)) break;
           if (!since) since = wall_clock64();
           else if (wall_clock64() - since > patience) break;
         }
-        if (lacks) {
-          if (lane == 0) told.lack = (uint32_t)__builtin_ctzll(lacks);
-        } else {
+        if (lane == 0) told.lack = lack;
+        if (lack == kVerifyChunks) {
           // ---- the row's sums over its chunks, and the node's children
           int32_t c = kNoDistribution;
           double m;
           if (!rest) {
-            const float mc = lane < p.chunks ? part_max[lane] : -INFINITY, most = wave_max_dpp(mc);
-            const bool none = __any(mc != mc) || most == -INFINITY;
+            float mc = part_max[0];
+            bool none = part_max[0] != part_max[0];
+#pragma unroll
+            for (uint32_t h = 1; h < kVerifyEach; ++h) { mc = fmaxf(mc, part_max[h]); none |= part_max[h] != part_max[h]; }
+            const float most = wave_max_dpp(mc);
             m = (double)most;
-            now = mc > -INFINITY ? part_sum[lane] * weight(mc, m, k) : 0.;
-            mass = wave_sum64(now);
+            double s = 0.;
+            uint32_t place = 0xFFFFFFFFu;
+#pragma unroll
+            for (uint32_t h = 0; h < kVerifyEach; ++h) {
+              now[h] = part_max[h] > -INFINITY ? part[h] * weight(part_max[h], m, k) : 0.;
+              s += now[h];
+              if (part_max[h] == most) place = min(place, part_place[h]);
+            }
+            mass = wave_sum64(s);
             drawn = 0.;
-            const uint32_t largest = greedy ? wave_min_u32(mc == most && lane < p.chunks ? part_place[lane] : 0xFFFFFFFFu) : 0u;
+            const uint32_t largest = greedy ? wave_min_u32(place) : 0u;
             if (lane == 0) {
               top[at] = most;
               total[at] = mass;
               told.place = largest;
             }
-            if (!none) c = !DRAFT || greedy ? try_chosen(at, near, m, largest, mass, now) : kRefused;
+            if (!__any(none) && most > -INFINITY) c = !DRAFT || greedy ? try_chosen(at, near, m, largest, mass, now) : kRefused;
           } else {
             m = (double)top[at];
-            const double part = lane < p.chunks ? part_sum[lane] : 0., s = wave_sum64(part);
-            if (s > 0.) { mass = s; now = part; }
-            else --subtracted;   // (nothing would be left: as it was)
+            double s = 0.;
+#pragma unroll
+            for (uint32_t h = 0; h < kVerifyEach; ++h) s += part[h];
+            s = wave_sum64(s);
+            if (s > 0.) {
+              mass = s;
+#pragma unroll
+              for (uint32_t h = 0; h < kVerifyEach; ++h) now[h] = part[h];
+            } else --subtracted;   // (nothing would be left: as it was)
             c = kRefused;
           }
           if (DRAFT && c == kRefused) {
@@ -463,7 +499,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
               told.subtracted = subtracted;
             }
           }
-          if (lane == 0) { told.code = c; told.lack = kVerifyChunks; }
+          if (lane == 0) told.code = c;
         }
       }
       __syncthreads();
@@ -480,18 +516,19 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     rest = DRAFT && ended == kRefused;
     if (rest) {
       ++subtracted;
-      there = false;
       continue;
     }
     if (ended < 0) break;
-    there = there && (uint32_t)ended == next_guess;
     at = (uint32_t)ended;
     child = at & ~63u;
     subtracted = 0;
     if (threadIdx.x == 0) path[length] = (uint8_t)at;
     ++length;
   }
-  if (wave == 0) part_sum[lane] = now;
+  if (wave == 0) {
+#pragma unroll
+    for (uint32_t h = 0; h < kVerifyEach; ++h) part_sum[64u * h + lane] = now[h];
+  }
   __syncthreads();
 
   // ---- the end of the walk: the token that follows is drawn from what is left of the last node's row, in the first chunk that ends beyond
@@ -500,11 +537,27 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   uint32_t chunk = 0;
   double goal = 0.;
   auto choose = [&]() {
-    double all;
-    const double mine = part_sum[lane], before = wave_before64(mine, &all);
-    const uint64_t any = __ballot(mine > 0.), beyond = __ballot(mine > 0. && before + mine > uniform * all);
-    chunk = beyond ? (uint32_t)__builtin_ctzll(beyond) : any ? 63u - (uint32_t)__builtin_clzll(any) : kVerifyChunks;
-    goal = uniform * all - lane64(before, chunk & 63u);
+    double front = 0.;   // (the lanes' first chunks, then their second ones)
+    double before[kVerifyEach], mine[kVerifyEach];
+#pragma unroll
+    for (uint32_t h = 0; h < kVerifyEach; ++h) {
+      double all;
+      mine[h] = part_sum[64u * h + lane];
+      before[h] = front + wave_before64(mine[h], &all);
+      front += all;
+    }
+    const double aim = uniform * front;
+    uint32_t beyond = kVerifyChunks, last = kVerifyChunks;
+#pragma unroll
+    for (uint32_t h = kVerifyEach; h-- > 0;) {
+      const uint64_t any = __ballot(mine[h] > 0.), set = __ballot(mine[h] > 0. && before[h] + mine[h] > aim);
+      if (set) beyond = 64u * h + (uint32_t)__builtin_ctzll(set);
+      if (any && last == kVerifyChunks) last = 64u * h + 63u - (uint32_t)__builtin_clzll(any);
+    }
+    chunk = beyond != kVerifyChunks ? beyond : last;
+#pragma unroll
+    for (uint32_t h = 0; h < kVerifyEach; ++h)
+      if (chunk >> 6 == h) goal = aim - lane64(before[h], chunk & 63u);
   };
   if (draws) choose();
   if (own == (chunk == kVerifyChunks ? 0u : chunk)) {
@@ -513,12 +566,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     const uint32_t here = threadIdx.x < length ? path[threadIdx.x] : 0u;
     if (a.logprobs && threadIdx.x + 1u < length) said = logit_of(row_of(here), (size_t)as_global(a.tokens)[begin + path[threadIdx.x + 1u]]);
     int32_t token = ended == kNone && greedy ? (int32_t)told.place : -1;
+    float logit = 0.f;   // the token's
     if (draws) {
       int32_t gone = -1;   // a child's token of the node: refused, as all of them are
       if (!DRAFT && threadIdx.x < nodes && threadIdx.x > at && as_global(a.parents)[begin + threadIdx.x] == (int32_t)at) gone = token_of(threadIdx.x);
       for (; chunk != kVerifyChunks; choose()) {
-        if (threadIdx.x == 0) { found[0] = 0xFFFFFFFFu; found[1] = 0; }
+        if (lane == 0) { hit[wave] = 0xFFFFFFFFu; last[wave] = 0; }
         double front = 0.;
+        uint32_t late = 0;   // the last token that has anything, + 1
         for (uint32_t step = 0; step < p.steps; ++step) {
           const uint32_t v0 = chunk * chunk_logits + step * kVerifyStep, v = v0 + threadIdx.x * kVerifyLane;
           float z[kVerifyLane];
@@ -535,13 +590,19 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
           double r[kVerifyLane], s = 0.;
           const double m = (double)top[at];
 #pragma unroll
-          for (uint32_t j = 0; j < kVerifyLane; ++j) {
-            r[j] = weight(y[j], m, k);
-            if constexpr (DRAFT) {
-              for (uint32_t i = 0; i < subtracted; ++i) r[j] = fmax(0., r[j] * over[i] - (double)z[j] * scale[i]);
-            } else r[j] = zero >> j & 1u ? 0. : r[j];
-            s += r[j];
+          for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = weight(y[j], m, k);
+          if constexpr (DRAFT) {
+            for (uint32_t i = 0; i < subtracted; ++i) {
+              const double o = over[i], f = scale[i];
+#pragma unroll
+              for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = fmax(0., r[j] * o - (double)z[j] * f);
+            }
+          } else {
+#pragma unroll
+            for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = zero >> j & 1u ? 0. : r[j];
           }
+#pragma unroll
+          for (uint32_t j = 0; j < kVerifyLane; ++j) s += r[j];
           double all, before = wave_before64(s, &all);
           if (lane == 0) sums[wave] = all;
           __syncthreads();
@@ -553,24 +614,36 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
           }
           const bool crosses = s > 0. && before + s > goal;
           const uint64_t any = __ballot(s > 0.), cross = __ballot(crosses);
-          // the wavefront's first thread that ends beyond the goal, or its last that has anything
+          // the wavefront's first thread that ends beyond the goal, or its last that has anything: a token and its logit
           if (any && lane == (cross ? (uint32_t)__builtin_ctzll(cross) : 63u - (uint32_t)__builtin_clzll(any))) {
-            uint32_t last = 0, hit = 0xFFFFFFFFu;
+            uint32_t which = 0xFFFFFFFFu;
+            float logit = 0.f;
+            bool over_it = false;
             double sum = before;
 #pragma unroll
             for (uint32_t j = 0; j < kVerifyLane; ++j) {
               sum += r[j];
-              const uint32_t place_j = row_start(v + j / E * E, a.vocab, E) + j % E;
-              last = r[j] > 0. ? place_j : last;
-              hit = r[j] > 0. && sum > goal && hit == 0xFFFFFFFFu ? place_j : hit;
+              if (r[j] > 0. && !over_it) {
+                which = row_start(v + j / E * E, a.vocab, E) + j % E;
+                logit = y[j];
+                over_it = crosses && sum > goal;
+              }
             }
-            if (crosses) atomicMin(&found[0], min(hit, last));
-            atomicMax(&found[1], last + 1u);
+            (crosses ? hit : last)[wave] = crosses ? which : which + 1u;
+            hit_logit[wave] = logit;
           }
           __syncthreads();
-          if (found[0] != 0xFFFFFFFFu) break;
+          token = -1;
+#pragma unroll
+          for (uint32_t i = 0; i < kVerifyWaves; ++i)
+            if (token < 0 && hit[i] != 0xFFFFFFFFu) { token = (int32_t)hit[i]; logit = hit_logit[i]; }
+          if (token >= 0) break;
+#pragma unroll
+          for (uint32_t i = 0; i < kVerifyWaves; ++i)
+            if (last[i] > late) { late = last[i]; logit = hit_logit[i]; }
+          __syncthreads();
         }
-        token = found[0] != 0xFFFFFFFFu ? (int32_t)found[0] : (int32_t)found[1] - 1;
+        if (token < 0) token = (int32_t)late - 1;
         if (token >= 0) break;
         if (threadIdx.x == 0) part_sum[chunk] = 0.;   // (a sum that was rounding alone)
         __syncthreads();
@@ -580,7 +653,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       as_global(a.lengths)[seq] = (int32_t)length;
       as_global(a.next)[seq] = token;
     }
-    if (a.logprobs && threadIdx.x + 1u == length && token >= 0) said = logit_of(row_of(at), (size_t)token);
+    if (threadIdx.x + 1u == length && token >= 0) said = greedy ? top[at] : logit;
     if (threadIdx.x < nodes) {
       const uint32_t t = threadIdx.x;
       as_global(a.path)[begin + t] = t < length ? (int32_t)here : -1;
