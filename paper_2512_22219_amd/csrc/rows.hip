@@ -176,6 +176,7 @@ constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
 constexpr float kAttendShare = 1.8e-4f;      // ... and a row's partial result
+constexpr float kTreeShare = 1.8e-4f;        // the same of trees
 constexpr uint32_t kJoinWorkgroups = 1024;
 // Rows and heads, up to as many as there are compute units, that get a workgroup each in the join (a wavefront / a workgroup each: 1 token
 // over 30000, 32 heads of 128, 30.6 / 26.0 us; 5 over 30000 of 64 20.1 / 17.9; 8 over 8000, 256 of them, 18.4 / 17.0; 512 18.8 / 19.3; 1024 14.7 / 16.7).
@@ -231,7 +232,7 @@ __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d) {
 __device__ __forceinline__ uint32_t first_tile_of_run(uint32_t k, uint32_t blocks, uint32_t pos, uint32_t lg) {
   return ((k * blocks * kBlockKeys - pos) << lg) / kTileRows;
 }
-template <int D, bool ONCE>   // ONCE: no sequence has more than one tile
+template <int D, bool ONCE, bool TREE>   // ONCE: no sequence has more than one tile
 __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, uint32_t lg) {
   const uint32_t lane = threadIdx.x & 63u, T = (uint32_t)(q.end - q.begin), rows = T << lg;
   auto add = [](auto x, auto y) { return x + y; };
@@ -256,12 +257,19 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
   // 17.6 us, eight times 200 over 300 51 / 24; tiles of up to 22 blocks never cut / as here: 64 tokens over 1000 27.6 / 15.3.)
   const uint32_t held = min(rows, kTileRows);
   const float share = (float)few * (float)held * kAttendShare;
-  c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
+  if constexpr (TREE) {
+    // Trees end together, with the longest run of all: one length for all of them, by all partial results, and cut or not at once.
+    const float parts = row16_reduce((float)rows * (float)nb, add) * (float)s.n_kv * kTreeShare;   // of runs of one block
+    const float longest = (float)row16_reduce(nb, [](uint32_t x, uint32_t y) { return max(x, y); });
+    c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf(parts));
+    c = uniform_u32(c);
+    if (uniform_f32(longest - (float)c - parts * __builtin_amdgcn_rcpf((float)c)) < (float)kAttendJoinBlocks) c = max(c, uniform_u32((uint32_t)longest));
+  } else c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
   if (ONCE) c = max(c, (nb + kAttendFewChunks - 1u) / kAttendFewChunks);
   for (;; c *= 2u) {   // (long enough that the partial results fit the workspace, and a tile's weights the LDS of the join)
     d.chunks = quotient(nb + c - 1u, c);
     const float saved = (float)nb - (float)c - share * (float)d.chunks;
-    if (saved < (ONCE && __any(saved >= (float)kAttendJoinBlocks) ? 0.f : (float)kAttendJoinBlocks)) d.chunks = 1u;
+    if (!TREE && saved < (ONCE && __any(saved >= (float)kAttendJoinBlocks) ? 0.f : (float)kAttendJoinBlocks)) d.chunks = 1u;
     const bool cut = T && d.chunks > 1u;
     const float need = cut ? (float)d.tiles * (float)d.chunks * (float)s.n_kv * (float)(held * (D + 2u)) : 0.f;
     if (uniform_f32(row16_reduce(need, add)) <= 0.99f * (float)(MPK_ROWS_WORKSPACE_BYTES / 4u) && __all(d.chunks <= kAttendMostChunks)) break;
@@ -375,7 +383,7 @@ __device__ __forceinline__ void attend_units(const AttendArgs& a, uint32_t lg) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tiles_lds;
   __builtin_amdgcn_s_setprio(3);   // (until the unit's first requests are out: 8 x 1 token 20.3 / 19.6 us)
   const SeqLanes q = load_seqs<TREE>(s, blockIdx.x == 0 && wave == 0);
-  const Deal d = deal_units<D, ONCE>(s, q, lg);
+  const Deal d = deal_units<D, ONCE, TREE>(s, q, lg);
   const uint32_t total = uniform_u32(d.total);
   if (blockIdx.x == 0 && threadIdx.x < kMaxRowSeqs) {   // what the join needs of it
     MPK_GLOBAL u32x4* to = as_global((u32x4*)a.work) + 2u * threadIdx.x;
