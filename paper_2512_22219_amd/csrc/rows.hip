@@ -176,7 +176,8 @@ constexpr uint32_t kTileRows = 128, kBlockKeys = 64;
 constexpr uint32_t kAttendMinBlocks = 3, kAttendMostChunks = 256;   // blocks of a run at least, runs of a tile at most
 constexpr uint32_t kAttendJoinBlocks = 5;   // what the join costs, in blocks
 constexpr float kAttendShare = 1.8e-4f;      // ... and a row's partial result
-constexpr float kTreeShare = 1.8e-4f;        // the same of trees
+constexpr float kTreeShare = 1.8e-4f;        // the same of trees (0.45e-4 / here / 4e-4: 4 x 256 nodes over 12000 462 / 377 / 376 us, 16 over 8000 16.9 / 17.3 / 19.9)
+constexpr uint32_t kComputeUnits = 256;
 constexpr uint32_t kJoinWorkgroups = 1024;
 // Rows and heads, up to as many as there are compute units, that get a workgroup each in the join (a wavefront / a workgroup each: 1 token
 // over 30000, 32 heads of 128, 30.6 / 26.0 us; 5 over 30000 of 64 20.1 / 17.9; 8 over 8000, 256 of them, 18.4 / 17.0; 512 18.8 / 19.3; 1024 14.7 / 16.7).
@@ -263,6 +264,9 @@ __device__ __forceinline__ Deal deal_units(const RowSeqs& s, const SeqLanes& q, 
     const float longest = (float)row16_reduce(nb, [](uint32_t x, uint32_t y) { return max(x, y); });
     c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf(parts));
     c = uniform_u32(c);
+    // A few units more than compute units would leave some of these with two, and the join waiting for them (22 nodes over 14600 29.1 / 25.5 us).
+    const uint32_t units = uniform_u32(row16_reduce(d.tiles * quotient(nb + c - 1u, c), add)) * s.n_kv;
+    if (units > kComputeUnits && units <= kComputeUnits * 4u / 3u) c = (c * units + kComputeUnits - 1u) / kComputeUnits;
     if (uniform_f32(longest - (float)c - parts * __builtin_amdgcn_rcpf((float)c)) < (float)kAttendJoinBlocks) c = max(c, uniform_u32((uint32_t)longest));
   } else c = max(min(max(c, kAttendMinBlocks), 1u << 22), 1u + (uint32_t)__builtin_amdgcn_sqrtf((float)nb * share));
   if (ONCE) c = max(c, (nb + kAttendFewChunks - 1u) / kAttendFewChunks);
@@ -369,10 +373,14 @@ __device__ __forceinline__ uint64_t bits_from(const uint64_t* bits, int32_t o) {
 constexpr uint32_t attend_lds(uint32_t D) { return 4u * kBlockKeys * D * 2u + 16u; }
 constexpr uint32_t tree_attend_lds(uint32_t D) { return attend_lds(D) + kTreeNodes * (kTreeNodes / 8u + 2u); }
 
-// ONCE: no sequence has more than one tile, so that a unit's keys are its own.  TREE: a row sees the cached rows, its ancestors in the
-// call's tree and itself, where another sees all in front of it and itself.
-template <int D, bool PAGED, bool ONCE, bool TREE>
-__device__ __forceinline__ void attend_units(const AttendArgs& a, uint32_t lg) {
+// ONCE: no sequence has more than one tile, so that a unit's keys are its own.  A tree's row sees the cached rows, its ancestors in the
+// call's tree and itself, where another sees all in front of it and itself.  (Which of the two is a type, whose name a trace then shows; one
+// function that two kernels inline is scheduled otherwise: 2048 tokens over 14000 885 / 893 us.)
+struct rows_attend_kernel { static constexpr bool kTree = false; };
+struct tree_attend_kernel { static constexpr bool kTree = true; };
+template <int D, bool PAGED, bool ONCE, typename KIND>
+__global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a, uint32_t lg) {
+  constexpr bool TREE = KIND::kTree;
   constexpr uint32_t KS = D / 16, NT = D / 32, CPR = D / 8, RPI = 64 / CPR, IPW = 16 / RPI, ROWB = D * 2, TILE = kBlockKeys * ROWB;
   extern __shared__ __align__(16) unsigned char tiles_lds[];   // K, V of the even blocks, K, V of the odd ones, a flag
   uint32_t& flag = *(uint32_t*)(tiles_lds + 4u * TILE);
@@ -651,11 +659,6 @@ __device__ __forceinline__ void attend_units(const AttendArgs& a, uint32_t lg) {
   }
 }
 
-template <int D, bool PAGED, bool ONCE>
-__global__ void __launch_bounds__(256, 2) rows_attend_kernel(AttendArgs a, uint32_t lg) { attend_units<D, PAGED, ONCE, false>(a, lg); }
-template <int D, bool PAGED, bool ONCE>
-__global__ void __launch_bounds__(256, 2) tree_attend_kernel(AttendArgs a, uint32_t lg) { attend_units<D, PAGED, ONCE, true>(a, lg); }
-
 // Joins the partial results of a row whose tile was cut into runs, in their order: W wavefronts per row and query head, every W-th
 // run each.
 template <int D, uint32_t W>
@@ -746,11 +749,11 @@ hipError_t rows_prepare(int device) {
   std::lock_guard<std::mutex> lock(mu);
   if ((size_t)device < done.size() && done[device]) return hipSuccess;
   hipError_t e = hipSuccess;
-  for (const void* fn : {(const void*)rows_attend_kernel<128, false, false>, (const void*)rows_attend_kernel<128, true, false>,
-                         (const void*)rows_attend_kernel<128, false, true>, (const void*)rows_attend_kernel<128, true, true>})
+  for (const void* fn : {(const void*)attend_kernel<128, false, false, rows_attend_kernel>, (const void*)attend_kernel<128, true, false, rows_attend_kernel>,
+                         (const void*)attend_kernel<128, false, true, rows_attend_kernel>, (const void*)attend_kernel<128, true, true, rows_attend_kernel>})
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_lds(128));
-  for (const void* fn : {(const void*)tree_attend_kernel<128, false, false>, (const void*)tree_attend_kernel<128, true, false>,
-                         (const void*)tree_attend_kernel<128, false, true>, (const void*)tree_attend_kernel<128, true, true>})
+  for (const void* fn : {(const void*)attend_kernel<128, false, false, tree_attend_kernel>, (const void*)attend_kernel<128, true, false, tree_attend_kernel>,
+                         (const void*)attend_kernel<128, false, true, tree_attend_kernel>, (const void*)attend_kernel<128, true, true, tree_attend_kernel>})
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tree_attend_lds(128));
   if (e == hipSuccess) {
     done.resize(std::max(done.size(), (size_t)device + 1u));
@@ -763,8 +766,8 @@ template <int D, bool PAGED, bool TREE>
 static hipError_t launch_attend(const AttendArgs& a, uint32_t lg, hipStream_t stream) {
   auto run = [&](uint32_t grid, auto once) {
     constexpr bool ONCE = decltype(once)::value;
-    if constexpr (TREE) tree_attend_kernel<D, PAGED, ONCE><<<dim3(grid), dim3(256), tree_attend_lds(D), stream>>>(a, lg);
-    else rows_attend_kernel<D, PAGED, ONCE><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
+    if constexpr (TREE) attend_kernel<D, PAGED, ONCE, tree_attend_kernel><<<dim3(grid), dim3(256), tree_attend_lds(D), stream>>>(a, lg);
+    else attend_kernel<D, PAGED, ONCE, rows_attend_kernel><<<dim3(grid), dim3(256), attend_lds(D), stream>>>(a, lg);
   };
   // units: one per tile, and up to kAttendSlots more where tiles are cut (a workgroup without one has worked that out for nothing;
   // one takes several where there are more)
