@@ -78,7 +78,6 @@ struct VerifyArgs {
   const float *temperatures, *uniforms;   // null: greedy
   int32_t *lengths, *path, *next;
   float* logprobs;   // or null
-  void* work;
   uint32_t* err;
   VerifySync* sync;   // [n_seqs]
   bool jitter;        // delays at random (MPK_DEBUG_JITTER)

@@ -1159,6 +1159,17 @@ static mpk_status rows_words(const char* name, const void* p) {   // (NULL where
   if ((uintptr_t)p % 4) { set_error("%s is not aligned to its elements", name); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
 }
+// Results where workgroups that are not through still read.
+static mpk_status rows_apart(std::initializer_list<std::pair<const char*, const void*>> results, std::initializer_list<std::pair<const char*, const void*>> lists) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (!r->second) continue;
+    for (const auto& l : lists)
+      if (l.second == r->second) { set_error("%s is %s", r->first, l.first); return MPK_ERR_INVALID_ARG; }
+    for (auto o = results.begin(); o != r; ++o)
+      if (o->second == r->second) { set_error("%s is %s", r->first, o->first); return MPK_ERR_INVALID_ARG; }
+  }
+  return MPK_OK;
+}
 constexpr uint32_t kRowsMost = 1u << 24;   // rows of a call
 constexpr uint32_t kRowsMostSeq = 1u << 28;   // max_seq of the graph
 constexpr uint32_t kRowsMostVocab = 1u << 30;   // vocab of a graph whose trees are verified
@@ -1337,6 +1348,9 @@ extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_
     if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
     if (draft_probs && draft_stride < vocab) { set_error("draft_probs: a row stride of %zu elements, the vocabulary has %u", draft_stride, vocab); return MPK_ERR_INVALID_ARG; }
     if ((st = rows_work(workspace)) != MPK_OK) return st;
+    if ((st = rows_apart({{"lengths", lengths}, {"path", path}, {"next_tokens", next_tokens}, {"logprobs", logprobs}},
+                         {{"row_begin", row_begin}, {"parents", parents}, {"tokens", tokens}, {"logits", logits}, {"draft_probs", draft_probs},
+                          {"temperatures", temperatures}, {"uniforms", uniforms}})) != MPK_OK) return st;
   }
   if ((st = rows_runnable(g)) != MPK_OK) return st;
   VerifyArgs a{};
@@ -1345,7 +1359,7 @@ extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_
   a.logits = logits; a.stride = row_stride; a.draft = draft_probs; a.draft_stride = draft_stride;
   a.temperatures = temperatures; a.uniforms = uniforms;
   a.lengths = lengths; a.path = path; a.next = next_tokens; a.logprobs = logprobs;
-  a.work = workspace; a.err = g->d_err; a.sync = g->d_verify; a.jitter = g->h.opt.debug_flags & MPK_DEBUG_JITTER;
+  a.err = g->d_err; a.sync = g->d_verify; a.jitter = g->h.opt.debug_flags & MPK_DEBUG_JITTER;
   HIP_TRY(launch_tree_verify(a, logits_type == MPK_ROWS_F32, (hipStream_t)stream));
   return MPK_OK;
 }
@@ -1358,7 +1372,7 @@ extern "C" mpk_status mpk_tree_keep(mpk_graph* g, uint32_t n_seqs, uint32_t n_ro
   if (st != MPK_OK) return st;
   if (n_rows && (!lengths || !path)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
   if ((st = rows_words("lengths", lengths)) != MPK_OK || (st = rows_words("path", path)) != MPK_OK || (st = rows_words("positions_out", positions_out)) != MPK_OK) return st;
-  if (positions_out == positions) { set_error("positions_out is positions"); return MPK_ERR_INVALID_ARG; }
+  if ((st = rows_apart({{"positions_out", positions_out}}, {{"row_begin", row_begin}, {"slots", slots}, {"positions", positions}, {"lengths", lengths}, {"path", path}})) != MPK_OK) return st;
   if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
   a.n_layers = g->h.cfg.n_layers;
   a.layer_stride = rows_of_layer(g->h) * a.s.n_kv * a.s.head_dim;

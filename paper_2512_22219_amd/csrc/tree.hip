@@ -20,7 +20,7 @@ constexpr uint32_t kVerifyLane = 8, kVerifyStep = kVerifyThreads * kVerifyLane; 
 constexpr uint32_t kVerifyEach = kVerifyChunks / 64;   // chunks of a lane when they are joined: the lane-th, the 64 + lane-th
 constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once
 constexpr uint32_t kVerifyPatience = 2000;   // ticks of 10 ns until others' sums are worked out
-
+constexpr uint32_t kVerifyTags = 1u << 30, kVerifyTagsJitter = 64u;   // rounds until tags start over (MPK_DEBUG_JITTER: often)
 
 struct VerifyPlan {
   uint32_t chunks, steps;   // of a row: a workgroup each; of a chunk
@@ -525,7 +525,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     if (threadIdx.x == 0) path[length] = (uint8_t)at;
     ++length;
   }
+  uint32_t left = 0;   // how many workgroups are through, their words (wavefront 0's stores) in place
   if (wave == 0) {
+    drain_vmem();
+    if (lane == 0) left = __hip_atomic_fetch_add(as_global(&sync.left), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
 #pragma unroll
     for (uint32_t h = 0; h < kVerifyEach; ++h) part_sum[64u * h + lane] = now[h];
   }
@@ -667,8 +670,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       }
     }
   }
-  // ---- who leaves last leaves the tag for the next call
-  if (threadIdx.x == 0 && __hip_atomic_fetch_add(as_global(&sync.left), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == p.chunks) {
+  // ---- who has been counted last leaves the tag for the next call.  Tags start over before they run out, with the words cleared: nobody looks
+  // at these any more.
+  if (wave || uniform_u32(left) != p.chunks) return;
+  if (tag >= (a.jitter ? kVerifyTagsJitter : kVerifyTags)) {
+    for (uint32_t i = lane; i < kVerifyDepth * kVerifyChunks * 8u; i += 64u) put64(&sync.word[0][0][0] + i, 0ull);
+    tag = 0;
+  }
+  if (lane == 0) {
     st_act_u32(&sync.left, 0u);
     st_act_u32(&sync.tag, tag);
   }

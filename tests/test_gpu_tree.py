@@ -1,5 +1,6 @@
 """mpk_tree_append, mpk_tree_attend and mpk_tree_keep on the GPU against 64-bit results, and the four calls together."""
 import random
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -586,3 +587,30 @@ def test_the_same_call_gives_the_same_bits_on_any_stream():
         outs.append(out)
     m.status()
     assert all(torch.equal(_bits(o), _bits(outs[0])) for o in outs)
+
+
+def test_a_graph_with_fewer_slots_than_its_cache_has():
+    """As a graph of a set: the same calls through a graph of two sequences on the cache of one of five leave the same bits in every layer."""
+    m = TreeModel(n_q=8, n_kv=2, d=64, batch=5, max_seq=512, layers=3)
+    ptrs = {n: t.data_ptr() for n, t in m.outer.items()}
+    ptrs["layers"] = [{n: t.data_ptr() for n, t in lw.items()} for lw in m.w]
+    shape, whole = SimpleNamespace(**dict(vars(m.shape), batch=2)), m.graph
+    part = M.compile_graph(shape, ptrs, (m.k.data_ptr(), m.v.data_ptr()), fusion=31, transitive_reduction=1, kv_batch=5)
+    lens, pos, begin, work = [90, 40], [300, 17], [0, 90, 130], workspace()
+    flat, _ = _forest(lens, ["random"] * 2, seed=3)
+    x, k0, v0, got = m.normal(130, 12 * 64), m.k.clone(), m.v.clone(), []
+    path, lengths = [0, 2, 50, 89] + [-1] * 86 + [1, 39] + [-1] * 38, [4, 2]
+    for graph in (whole, part):
+        m.graph = graph
+        m.k.copy_(k0), m.v.copy_(v0)
+        outs = []
+        for layer in range(3):
+            q, out = (torch.zeros(130, 512, dtype=torch.bfloat16, device=m.dev) for _ in range(2))
+            m.tree_append(layer, begin, [1, 0], pos, flat, x, q)
+            m.tree_attend(layer, begin, [1, 0], pos, flat, q, out, work)
+            outs += [q, out]
+        m.keep(begin, [1, 0], pos, lengths, path)
+        m.status()
+        got.append(outs + [m.k.clone(), m.v.clone()])
+    assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(*got))
+    assert not torch.equal(_bits(got[0][-1]), _bits(v0))

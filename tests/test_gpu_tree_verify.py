@@ -60,7 +60,7 @@ def _check(m, begin, parents, tokens, logits, out, temperatures, uniforms, draft
     assert (path[~mine] == 77).all() and (lp[~mine] == 77).all()
 
 
-def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperatures=None, first=0, behind=0, pad=0, std=2.0, batch=16, masked=0.0, **opts):
+def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperatures=None, first=0, behind=0, pad=0, std=2.0, batch=16, masked=0.0, calls=1, **opts):
     gen = torch.Generator().manual_seed(seed)
     m = TreeModel(n_q=2, n_kv=1, batch=batch, max_seq=8, vocab=vocab, layers=1, **opts)
     begin = _begin(lens, first)
@@ -91,9 +91,10 @@ def _case(seed, vocab, lens, kinds, dtype=torch.float32, draft=None, temperature
     if q is not None:
         dwide = torch.full((rows, vocab + pad), float("nan"), device=dev)
         dwide[:, :vocab] = q.to(dev)
-    out = m.verify(begin, parents, tokens, wide, workspace(), draft=dwide, once=once, temperatures=temps, uniforms=None if temps is None else uniforms)
-    m.status()
-    _check(m, begin, parents, tokens, logits, out, temps, uniforms, q, once)
+    for _ in range(calls):
+        out = m.verify(begin, parents, tokens, wide, workspace(), draft=dwide, once=once, temperatures=temps, uniforms=None if temps is None else uniforms)
+        m.status()
+        _check(m, begin, parents, tokens, logits, out, temps, uniforms, q, once)
     return out
 
 
@@ -117,6 +118,22 @@ def test_workgroups_that_are_late(draft, seed):
     """Every workgroup waits at random, in each round, up to twice as long as the others wait for it: the same tokens."""
     for dtype in (torch.float32, torch.bfloat16):
         _case(seed, 70001, [9, 1, 30], ["chain", "chain", "random"], dtype, draft, [1.0, 0.0, 0.8], debug_flags=M.DEBUG_JITTER)
+
+
+@pytest.mark.parametrize("draft", [None, "drawn", "once"])
+@pytest.mark.parametrize("vocab,lens,dtype", [(100003, [3, 9, 1, 0, 6, 2, 4, 5, 1, 7, 3, 3, 2, 8, 1, 5], torch.bfloat16),
+                                              (100003, [3, 9, 1, 0, 6, 2, 4, 5, 1, 7, 3, 3, 2, 8, 1, 5], torch.float32),
+                                              (262144, [6, 3], torch.float32), (262145, [6], torch.bfloat16), (600001, [5], torch.float32)])
+def test_verify_rows_of_several_steps_a_workgroup(vocab, lens, dtype, draft):
+    """More logits than a workgroup takes at once: many sequences, or more than the largest number of chunks."""
+    kinds = [("chain", "star", "random")[i % 3] for i in range(len(lens))]
+    _case(vocab + len(lens), vocab, lens, kinds, dtype, draft, [1.0, 0.0, 0.7], pad=1)
+
+
+@pytest.mark.parametrize("draft", [None, "drawn"])
+def test_many_workgroups_that_are_late_on_one_graph(draft):
+    """As above with every sequence a call can have, call after call on one graph: words of earlier rounds are there, and start over."""
+    _case(1, 40001, [5, 1, 7, 3, 0, 9, 2, 4, 6, 1, 3, 8, 2, 5, 7, 4], ["random"] * 16, torch.float32, draft, [1.0, 0.0, 0.8], calls=8, debug_flags=M.DEBUG_JITTER)
 
 
 @pytest.mark.parametrize("draft", [None, "once"])
@@ -356,3 +373,41 @@ def test_the_same_call_gives_the_same_bits_two_graphs_at_once():
     for g, w in zip(got, want):
         for out in g:
             assert all(torch.equal(a, b) for a, b in zip(out, w))
+
+
+def test_replays_between_other_calls_on_the_graph():
+    """A captured call, replayed with new trees, logits and numbers, between calls of another number of sequences (other chunks) on the
+    same graph, and after a reset."""
+    V = 60000
+    m = TreeModel(n_q=2, n_kv=1, batch=8, max_seq=8, vocab=V, layers=1)
+    gen, work = torch.Generator().manual_seed(6), workspace()
+    lens = [7, 12, 3]
+    begin = _begin(lens)
+    ints = [m.ints(x) for x in (begin, [-1] * 22, [0] * 22)]
+    x, u, heat = torch.zeros(22, V, device="cuda"), torch.zeros(22, device="cuda"), torch.tensor([1.0, 0.0, 0.6], device="cuda")
+    out = [m.ints([77] * 3), m.ints([77] * 22), m.ints([77] * 3), torch.full((22,), 77.0, device="cuda")]
+
+    def call(stream):
+        m.graph.tree_verify(3, 22, ints[0].data_ptr(), ints[1].data_ptr(), ints[2].data_ptr(), x.data_ptr(), M.ROWS_F32, V, 0, 0, 0, heat.data_ptr(), u.data_ptr(),
+                            *[t.data_ptr() for t in out], work.data_ptr(), stream)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(torch.cuda.current_stream().cuda_stream)
+    for n in range(6):
+        parents = sum((tree(k, "random", 10 * n + i) for i, k in enumerate(lens)), [])
+        logits, uniforms = torch.randn(22, V, generator=gen) * 2, torch.rand(22, generator=gen)
+        logits[torch.arange(22), torch.randint(V, (22,), generator=gen)] += 14
+        tokens = _tokens(gen, logits, parents, begin, None, False, None)
+        ints[1].copy_(m.ints(parents)), ints[2].copy_(m.ints(tokens)), x.copy_(logits), u.copy_(uniforms)
+        for t in out:
+            t.fill_(77)
+        graph.replay()
+        m.status()
+        _check(m, begin, parents, tokens, logits, out, heat.tolist(), uniforms)
+        sub = slice(begin[n % 3], begin[n % 3 + 1])   # one of the sequences alone, its row in chunks of its own
+        alone = m.verify([0, lens[n % 3]], parents[sub], tokens[sub], x[sub].clone(), work, temperatures=[1.0], uniforms=uniforms[sub])
+        m.status()
+        _check(m, [0, lens[n % 3]], parents[sub], tokens[sub], logits[sub], alone, [1.0], uniforms[sub])
+        if n == 3:
+            m.graph.reset()

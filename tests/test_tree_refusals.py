@@ -5,6 +5,7 @@ import paper_2512_22219_amd as M
 from tests.rows_util import RowsModel
 
 P = 1 << 20   # an aligned address that nothing reads
+R = [P + 4096 * (i + 1) for i in range(4)]   # ... and others
 
 
 @pytest.fixture(scope="module")
@@ -21,8 +22,8 @@ def _refused(call, *args, match, status=M.MPK_ERR_INVALID_ARG):
 APPEND = dict(layer=0, n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, parents=P, qkv=P, kind=0, stride=512, q=P + 512, q_stride=256)
 ATTEND = dict(layer=0, n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, parents=P, q=P, q_stride=256, out=P + 512, out_stride=256, work=P)
 VERIFY = dict(n_seqs=1, n_rows=5, begin=P, parents=P, tokens=P, logits=P, kind=1, stride=64, draft=P, draft_stride=64, flags=0,
-              temperatures=P, uniforms=P, lengths=P, path=P, next=P, logprobs=P, work=P)
-KEEP = dict(n_seqs=1, n_rows=5, begin=P, slots=0, positions=P, lengths=P, path=P, out=P + 512)
+              temperatures=P, uniforms=P, lengths=R[0], path=R[1], next=R[2], logprobs=R[3], work=P)
+KEEP = dict(n_seqs=1, n_rows=5, begin=R[0], slots=0, positions=P, lengths=R[1], path=R[2], out=P + 512)
 
 
 @pytest.mark.parametrize("change,match", [
@@ -75,8 +76,30 @@ def test_keep(model, change, match):
     ("tree_keep", KEEP, "path", "path"), ("tree_keep", KEEP, "out", "positions_out")])
 def test_lists_and_results_off_their_elements(model, call, args, name, says, off):
     assert name in args
-    _refused(getattr(model.graph, call), *dict(args, **{name: P + off}).values(), match=f"^.*{says} is not aligned")
-    _refused(getattr(model.graph, call), *dict(args, **{name: P + 4}).values(), match="host_only")
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + 16 + off}).values(), match=f"^.*{says} is not aligned")
+    _refused(getattr(model.graph, call), *dict(args, **{name: P + 20}).values(), match="host_only")
+
+
+@pytest.mark.parametrize("result,on,match", [
+    ("lengths", "begin", "lengths is row_begin"), ("path", "parents", "path is parents"), ("path", "tokens", "path is tokens"),
+    ("next", "temperatures", "next_tokens is temperatures"), ("logprobs", "uniforms", "logprobs is uniforms"), ("logprobs", "logits", "logprobs is logits"),
+    ("logprobs", "draft", "logprobs is draft_probs"), ("path", "lengths", "path is lengths"), ("next", "path", "next_tokens is path"),
+    ("logprobs", "next", "logprobs is next_tokens")])
+def test_results_on_what_is_read(model, result, on, match):
+    apart = dict(VERIFY, **{n: P + 4096 * (i + 9) for i, n in enumerate(VERIFY) if VERIFY[n] == P})
+    _refused(model.graph.tree_verify, *apart.values(), match="host_only")
+    _refused(model.graph.tree_verify, *dict(apart, **{result: apart[on]}).values(), match=match)
+
+
+@pytest.mark.parametrize("on,name", [("begin", "row_begin"), ("slots", "slots"), ("positions", "positions"), ("lengths", "lengths"), ("path", "path")])
+def test_new_positions_on_what_is_read(model, on, name):
+    _refused(model.graph.tree_keep, *dict(KEEP, **{on: P + 512}).values(), match=f"positions_out is {name}")
+
+
+def test_a_vocabulary_too_large():
+    g = RowsModel(vocab=(1 << 30) + 8, host_only=True).graph
+    _refused(g.tree_verify, *VERIFY.values(), match="vocab", status=M.MPK_ERR_UNSUPPORTED)
+    _refused(g.tree_append, *APPEND.values(), match="host_only")   # (looks at no logits)
 
 
 def test_no_rows_need_no_buffers():
