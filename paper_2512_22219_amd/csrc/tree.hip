@@ -15,11 +15,23 @@ namespace mpk {
 // So a round is one pass over a chunk and one exchange between the compute units, and nobody waits for a decision to be passed on.
 // Nor does anybody depend on workgroups that may not run yet: sums that have not come after a while are worked out by
 // who needs them (the same operations in the same order, the same bits), so that each workgroup alone comes to the end.
+//
+// Bound by the latency of the rounds, one behind the other; a row of 150000 logits is read in a fraction of a microsecond.  A round of one sequence
+// takes 4.4 us: the chunk's logits 0.6 to 0.9, weights 0.5, sums over the workgroup 0.5, the exchange 1.4 to 1.8, the row's sums and the children 1;
+// beside the rounds 2 us at the start (lists, the root's row) and 3 to 4 where a token is drawn.  A chain of 6, greedy, 8 to 17 us by what
+// is accepted, 64 nodes 14 to 19, 8 x 25 drawn nodes over 128256 logits in bf16 31 to 48, 16 x 64 33 to 41.
+// A workgroup a sequence takes 81, 505, 650 and 653 us for these.  No better were: units handed out by a counter, whoever comes last deciding
+// (atomics on one address take 20 ns each: 64 nodes 30 us); several nodes of the tree in a round (1 / 2 / 3: 64 nodes 20.8 / 20.6 / 20.8, 8 x 25 drawn
+// 48 / 59 / 68, a chain of 6 8.5 to 17.4 / 10.4 to 17.3 / 11.6); the chunk of the child that is tried next requested while the others' sums come (no
+// change: the wait is for the slowest of all), or summed as well (16.7 / 16.8, 18.2 / 19.7, 34.8 / 37.3, 40.5 / 43.4).
 constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
-constexpr uint32_t kVerifyLane = 8, kVerifyStep = kVerifyThreads * kVerifyLane;   // logits of a thread and of a workgroup at once
+// Logits of a thread and of a workgroup at once.  Chunks of 2048 / 4096: 64 nodes 18.2 / 21.7 us, 8 x 25 drawn
+// 35.5 / 38.3.
+constexpr uint32_t kVerifyLane = 8, kVerifyStep = kVerifyThreads * kVerifyLane;
 constexpr uint32_t kVerifyEach = kVerifyChunks / 64;   // chunks of a lane when they are joined: the lane-th, the 64 + lane-th
-constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once
-constexpr uint32_t kVerifyPatience = 2000;   // ticks of 10 ns until others' sums are worked out
+constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once, three a compute unit
+// Ticks of 10 ns until others' sums are worked out: several rounds, so that it happens only where a workgroup does not run.
+constexpr uint32_t kVerifyPatience = 2000;
 constexpr uint32_t kVerifyTags = 1u << 30, kVerifyTagsJitter = 64u;   // rounds until tags start over (MPK_DEBUG_JITTER: often)
 
 struct VerifyPlan {
@@ -220,7 +232,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       float y[kVerifyLane];
 #pragma unroll
       for (uint32_t j = 0; j < kVerifyLane; ++j) y[j] = ahead[j];
-      if (step + 1u < p.steps) request(node, chunk, step + 1u, ahead);
+      if (step + 1u < p.steps) request(node, chunk, step + 1u, ahead);   // (one step ahead / not: 16 x 64 nodes 33 to 41 / 36 to 43 us)
       float mx = y[0];
 #pragma unroll
       for (uint32_t j = 0; j < kVerifyLane; ++j) {
@@ -368,6 +380,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
 
   // ---- the exchange: a chunk's sums in words that have the round's tag each (the place where something is greedy)
   const uint32_t words = greedy ? 4u : 3u;
+  // (a line of 64 bytes a chunk: side by side 8 x 25 drawn took 39 to 51 us, so 30 to 46)
   auto leave = [&](float m, double sum, uint32_t first) {
     if (lane < words) {
       const uint32_t v = lane == 0u ? __float_as_uint(m) : lane == 1u ? (uint32_t)__double2hiint(sum) : lane == 2u ? (uint32_t)__double2loint(sum) : first;
@@ -697,7 +710,8 @@ hipError_t launch_tree_verify(const VerifyArgs& a, bool f32, hipStream_t stream)
 // ------------------------------------------------------------------------------------ keep
 // The rows of a path, place t_k behind the cached rows, to place k.  t_k >= k and ascends, so a row that is written is never one still
 // to be read if they are moved in ascending order: a wavefront moves those of one layer, K or V, sequence and KV head, 16 (of 64
-// elements 32) at a time, all read before any is written.
+// elements 32) at a time, all read before any is written.  Bound by latency (lists, path, pages, rows, one behind the other): 5 of 32 nodes in 36
+// layers 3.4 us, 16 paths on pages, 9 MB read and written, 7.0 (a copy takes 1.8).  The path requested beside its length: 3.4, 7.1.
 template <int D>
 __global__ void __launch_bounds__(256) tree_keep_kernel(KeepArgs a) {
   constexpr uint32_t LPR = D / 8, RPI = 64 / LPR, N = 4;   // lanes of a row, rows of a load, loads in flight
