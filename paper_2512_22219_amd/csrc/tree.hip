@@ -23,7 +23,9 @@ namespace mpk {
 // A workgroup a sequence takes 81, 505, 650 and 653 us for these.  No better were: units handed out by a counter, whoever comes last deciding
 // (atomics on one address take 20 ns each: 64 nodes 30 us); several nodes of the tree in a round (1 / 2 / 3: 64 nodes 20.8 / 20.6 / 20.8, 8 x 25 drawn
 // 48 / 59 / 68, a chain of 6 8.5 to 17.4 / 10.4 to 17.3 / 11.6); the chunk of the child that is tried next requested while the others' sums come (no
-// change: the wait is for the slowest of all), or summed as well (16.7 / 16.8, 18.2 / 19.7, 34.8 / 37.3, 40.5 / 43.4).
+// change: the wait is for the slowest of all), or summed as well (16.7 / 16.8, 18.2 / 19.7, 34.8 / 37.3, 40.5 / 43.4), or that by four wavefronts while a
+// fifth leads (a round 4.3 / 3.5 where that child is accepted, but 0.5 more once: a chain of 6 8.1 to 16.7 / 8.5 to 15.6, 64 nodes 18.2 / 19.2, 8 x 25 35.5 / 37.4;
+// and two workgroups a compute unit instead of three); what is left of a chunk kept in LDS from one refused child to the next (no change; a star of 60: 48 / 42).
 constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
 // Logits of a thread and of a workgroup at once.  Chunks of 2048 / 4096: 64 nodes 18.2 / 21.7 us, 8 x 25 drawn
 // 35.5 / 38.3.
@@ -140,6 +142,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   __shared__ uint32_t places[kVerifyWaves], hit[kVerifyWaves], last[kVerifyWaves], zeros[kVerifyThreads];
   __shared__ struct { int32_t code; uint32_t lack, place, child, subtracted; } told;   // by wavefront 0
   __shared__ uint8_t path[kTreeNodes];
+  __shared__ int32_t tokens[kTreeNodes];   // -1: none; wavefront 0 has them at once, the others behind the first round
+  __shared__ float uniforms[kTreeNodes];
   const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), seq = blockIdx.x % a.n_seqs, own = blockIdx.x / a.n_seqs;   // its chunk
   VerifySync& sync = a.sync[seq];
 
@@ -171,6 +175,18 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   };
   if (!out) request(0u, own, 0u, y);
   TreeLanes tree;
+  int32_t token[kTreeNodes / 64u] = {};   // (on their way beside the parents: a round waits for the children's logits alone, 2 % of a call)
+  float number[kTreeNodes / 64u] = {};
+  if (wave == 0 && nodes <= kTreeNodes) {
+#pragma unroll
+    for (uint32_t i = 0; i < kTreeNodes / 64u; ++i) {
+      const uint32_t t = 64u * i + lane;
+      if (t > 0u && t < nodes) {
+        token[i] = as_global(a.tokens)[begin + t];
+        if (a.temperatures) number[i] = as_global(a.uniforms)[begin + t];
+      }
+    }
+  }
   if (nodes > kTreeNodes) {
     if (teller && lane == 0) report_rows(a.err, DE_BAD_TREE, seq, nodes);
     out = true;
@@ -184,14 +200,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     if (wrong < nodes) {
       if (teller && lane == 0) report_rows(a.err, DE_BAD_PARENT, seq, wrong);
       out = true;
-    } else if (teller) {
+    } else if (wave == 0) {
 #pragma unroll
       for (uint32_t i = 0; i < kTreeNodes / 64u; ++i) {
         const uint32_t t = 64u * i + lane;
-        if (t > 0u && t < nodes) {
-          const int32_t token = as_global(a.tokens)[begin + t];
-          if (token < 0 || (uint32_t)token >= a.vocab) report_rows(a.err, DE_BAD_TOKEN, seq, (uint32_t)token);
-        }
+        const bool fine = (uint32_t)token[i] < a.vocab;
+        if (!fine && teller) report_rows(a.err, DE_BAD_TOKEN, seq, (uint32_t)token[i]);
+        tokens[t] = fine ? token[i] : -1;
+        uniforms[t] = number[i];
       }
     }
     if (!(temperature >= 0.f && temperature < INFINITY)) {
@@ -215,10 +231,6 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   const double k = 1.4426950408889634 / (greedy ? 1. : (double)temperature);
   auto draft_of = [&](uint32_t node) { return a.draft + (size_t)(begin + node) * a.draft_stride; };
   auto parents_of = [&](uint32_t i) { return i == 0u ? tree.of[0] : i == 1u ? tree.of[1] : i == 2u ? tree.of[2] : tree.of[3]; };   // of the nodes 64 i + lane
-  auto token_of = [&](uint32_t t) {   // -1: none
-    const int32_t token = as_global(a.tokens)[begin + t];
-    return token < 0 || (uint32_t)token >= a.vocab ? -1 : token;
-  };
 
   // ---- a chunk of a node's row, by the workgroup: a wavefront's largest logit, its first place, and the sum of the weights against that; then, in
   // wavefront 0, the chunk's (in m a NaN: the row has no distribution).  The first step's logits may be there already.
@@ -320,10 +332,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   auto children_of = [&](uint32_t node, uint32_t i) {
     const uint32_t t = 64u * i + lane;
     Children c = {-1, 0.f, 0.f, 0.f};
-    if (t < nodes && parents_of(i) == (int32_t)node) c.token = token_of(t);
+    if (t < nodes && parents_of(i) == (int32_t)node) c.token = tokens[t];
     if (c.token >= 0 && !greedy) {
       c.x = logit_of(row_of(node), (size_t)c.token);
-      c.u = as_global(a.uniforms)[begin + t];
+      c.u = uniforms[t];
       if constexpr (DRAFT) c.q = as_global(draft_of(node))[c.token];
     }
     return c;
@@ -344,7 +356,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
         const uint32_t j = (uint32_t)__builtin_ctzll(set);
         const int32_t mine = __builtin_amdgcn_readlane(c.token, j);
         bool twin = lane < j && c.token == mine;   // of an earlier child: ruled out by now
-        for (uint32_t g = node >> 6; g < i; ++g) twin |= parents_of(g) == (int32_t)node && 64u * g + lane < nodes && token_of(64u * g + lane) == mine;
+        for (uint32_t g = node >> 6; g < i; ++g) twin |= parents_of(g) == (int32_t)node && 64u * g + lane < nodes && tokens[64u * g + lane] == mine;
         const double r = __any(twin) ? 0. : lane64(w, j), u = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c.u), j));
         if (u * mass < r) return (int32_t)(64u * i + j);
         if (mass - r > 0.) mass -= r;
@@ -580,12 +592,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     // (what the path's nodes say about the tokens behind them, a thread each: on its way meanwhile)
     float said = 0.f;
     const uint32_t here = threadIdx.x < length ? path[threadIdx.x] : 0u;
-    if (a.logprobs && threadIdx.x + 1u < length) said = logit_of(row_of(here), (size_t)as_global(a.tokens)[begin + path[threadIdx.x + 1u]]);
+    if (a.logprobs && threadIdx.x + 1u < length) said = logit_of(row_of(here), (size_t)tokens[path[threadIdx.x + 1u]]);
     int32_t token = ended == kNone && greedy ? (int32_t)told.place : -1;
     float logit = 0.f;   // the token's
     if (draws) {
       int32_t gone = -1;   // a child's token of the node: refused, as all of them are
-      if (!DRAFT && threadIdx.x < nodes && threadIdx.x > at && as_global(a.parents)[begin + threadIdx.x] == (int32_t)at) gone = token_of(threadIdx.x);
+      if (!DRAFT && threadIdx.x < nodes && threadIdx.x > at && as_global(a.parents)[begin + threadIdx.x] == (int32_t)at) gone = tokens[threadIdx.x];
       for (; chunk != kVerifyChunks; choose()) {
         if (lane == 0) { hit[wave] = 0xFFFFFFFFu; last[wave] = 0; }
         double front = 0.;
