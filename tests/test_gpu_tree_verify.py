@@ -411,3 +411,32 @@ def test_replays_between_other_calls_on_the_graph():
         _check(m, [0, lens[n % 3]], parents[sub], tokens[sub], logits[sub], alone, [1.0], uniforms[sub])
         if n == 3:
             m.graph.reset()
+
+
+@pytest.mark.parametrize("draft", [None, "once"])
+def test_beside_work_that_fills_the_gpu(draft):
+    """Products on another stream hold compute units, so that a call's workgroups do not all run at once: the same results, in time."""
+    V, lens = 120001, [9, 1, 14, 5, 0, 3, 7, 2]
+    m = TreeModel(n_q=2, n_kv=1, batch=8, max_seq=8, vocab=V, layers=1)
+    gen = torch.Generator().manual_seed(8)
+    begin, parents = _begin(lens), sum((tree(n, "random", i) for i, n in enumerate(lens)), [])
+    x = torch.randn(begin[-1], V, generator=gen) * 2
+    x[torch.arange(begin[-1]), torch.randint(V, (begin[-1],), generator=gen)] += 12
+    q = torch.softmax(x + torch.randn(begin[-1], V, generator=gen), 1) if draft else None
+    tokens, uniforms, temps = _tokens(gen, x, parents, begin, q, True, None), torch.rand(begin[-1], generator=gen), [1.0, 0.0, 0.8, 1.2] * 2
+    logits, probs, work = x.cuda(), q.cuda() if draft else None, workspace()
+    a, other = torch.randn(6000, 6000, device="cuda", dtype=torch.bfloat16), torch.cuda.Stream()
+    outs, keep = [], []
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(other):
+            for _ in range(4):
+                b = a @ a
+        for _ in range(3):
+            outs.append(m.verify(begin, parents, tokens, logits, work, probs, draft == "once", temps, uniforms))
+            keep.append(m.keep_alive)
+    torch.cuda.synchronize()
+    m.status()
+    for out in outs:
+        assert all(torch.equal(p.view(torch.int32), r.view(torch.int32)) for p, r in zip(out, outs[0]))
+    _check(m, begin, parents, tokens, x, outs[0], temps, uniforms, q, draft == "once")
