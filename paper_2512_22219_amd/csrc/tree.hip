@@ -26,7 +26,8 @@ namespace mpk {
 // change: the wait is for the slowest of all), or summed as well (16.7 / 16.8, 18.2 / 19.7, 34.8 / 37.3, 40.5 / 43.4), or that by four wavefronts while a
 // fifth leads (a round 4.3 / 3.5 where that child is accepted, but 0.5 more once: a chain of 6 8.1 to 16.7 / 8.5 to 15.6, 64 nodes 18.2 / 19.2, 8 x 25 35.5 / 37.4;
 // and two workgroups a compute unit instead of three); what is left of a chunk kept in LDS from one refused child to the next (no change; 13 trees of 55 nodes,
-// ten children a node, 48.4 / 42.1).
+// ten children a node, 48.4 / 42.1); a sequence's workgroups on one XCD (one over 150000 logits 16.7 / 21.0, 13 over 19000 58.3 / 55.3; where it
+// is no more than one a compute unit 0.6 % of 52 calls' mean).
 constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
 // Logits of a thread and of a workgroup at once.  Chunks of 2048 / 4096: 64 nodes 18.2 / 21.7 us, 8 x 25 drawn
 // 35.5 / 38.3.
