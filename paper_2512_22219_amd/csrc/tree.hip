@@ -9,8 +9,8 @@ namespace mpk {
 // ------------------------------------------------------------------------------------ verify
 // The walk needs, of each node that it comes to, the largest logit m and Z = sum 2^(k (x - m)), k = log2(e) / temperature, in 64 bits: a random
 // number is compared with sums of up to a vocabulary of weights, and which side it falls on is a token.
-// It goes in rounds.  A round is a node of the walk or, with a draft distribution, what is left of the node's distribution behind a refused
-// child.  A row is cut into chunks, one for each of the sequence's workgroups.  Each leaves its sums where all of them read
+// It goes in rounds.  A round is a node of the walk or what is left of the node's distribution behind refused children: with a draft
+// distribution behind each; of chosen tokens, whose weights are taken off the row's sum meanwhile, where hardly anything is left (kVerifyLeft).  A row is cut into chunks, one for each of the sequence's workgroups.  Each leaves its sums where all of them read
 // them, reads all of them, and works out for itself how the walk goes on.
 // So a round is one pass over a chunk and one exchange between the compute units, and nobody waits for a decision to be passed on.
 // Nor does anybody depend on workgroups that may not run yet: sums that have not come after a while are worked out by
@@ -36,6 +36,10 @@ constexpr uint32_t kVerifyEach = kVerifyChunks / 64;   // chunks of a lane when 
 constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once, three a compute unit
 // Ticks of 10 ns until others' sums are worked out: several rounds, so that it happens only where a workgroup does not run.
 constexpr uint32_t kVerifyPatience = 2000;
+// Refused chosen tokens are taken off the sums until less than this is left of them; then what is left is summed anew, against its own largest logit.
+// A difference has the sums' error, some 1e-13 of what they began with, so what is compared with random numbers and drawn from stays within 1e-10.  A
+// node comes to this with the same probability: its numbers have refused all the rest.
+constexpr double kVerifyLeft = 1. / 1024.;
 constexpr uint32_t kVerifyTags = 1u << 30, kVerifyTagsJitter = 64u;   // rounds until tags start over (MPK_DEBUG_JITTER: often)
 
 struct VerifyPlan {
@@ -47,22 +51,23 @@ enum : int32_t { kNone = -1, kNoDistribution = -2, kRefused = -3 };
 
 __device__ __forceinline__ void put64(uint64_t* p, uint64_t v) { __hip_atomic_store(as_global(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// 2^d for d <= 0, 0 below -1000 (and for -inf): a polynomial of degree 9 through the Chebyshev points of [-1/2, 1/2], within 1.9e-14 of the
-// value, and the power of two added to the exponent.
+// 2^d for d <= 0, 0 below -1000 (and for -inf): a polynomial p of degree 9 on [-1/2, 1/2], within 2.1e-14 of the value, and the power of two
+// added to the exponent.  p(0) = 1 exactly, p'(0) = ln 2: the points of p are +-sqrt(y), y the zeros of the Chebyshev polynomial of degree 5 over the
+// interval [0, 1/4] of squares, moved so that the least is 0.  So the weight of a row's largest logit is 1, however many sums it goes through.
 template <bool ZERO = true>   // false: d is not below -1000
 __device__ __forceinline__ double exp2_64(double d) {
   const double big = 6755399441055744.0;   // 1.5 x 2^52: the sum's low bits are d as a whole number
   const double t = d + big, f = d - (t - big);
-  double p = 0x1.b6571de2f2351p-24;
-  p = fma(p, f, 0x1.63ef969a64d3cp-20);
-  p = fma(p, f, 0x1.ffcb76789860fp-17);
-  p = fma(p, f, 0x1.43088e257f341p-13);
-  p = fma(p, f, 0x1.5d87fe908f88ap-10);
-  p = fma(p, f, 0x1.3b2ab72b175eep-7);
-  p = fma(p, f, 0x1.c6b08d7044119p-5);
-  p = fma(p, f, 0x1.ebfbdff8149f2p-3);
-  p = fma(p, f, 0x1.62e42fefa39f7p-1);
-  p = fma(p, f, 0x1.000000000003dp+0);
+  double p = 0x1.b64f6fecb838ep-24;
+  p = fma(p, f, 0x1.63e7f7eb368ffp-20);
+  p = fma(p, f, 0x1.ffcb7f06ad7afp-17);
+  p = fma(p, f, 0x1.430896a28d2bbp-13);
+  p = fma(p, f, 0x1.5d87fe8d66e50p-10);
+  p = fma(p, f, 0x1.3b2ab724d2acep-7);
+  p = fma(p, f, 0x1.c6b08d7045c65p-5);
+  p = fma(p, f, 0x1.ebfbdff81b648p-3);
+  p = fma(p, f, 0x1.62e42fefa39efp-1);
+  p = fma(p, f, 1.0);
   const uint32_t hi = (uint32_t)__double2hiint(p) + ((uint32_t)__double2loint(t) << 20);
   return ZERO && d < -1000. ? 0. : __hiloint2double((int)hi, __double2loint(p));
 }
@@ -142,7 +147,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   __shared__ double part_sum[kVerifyChunks], total[kTreeNodes], over[kTreeNodes], scale[kTreeNodes], sums[kVerifyWaves];
   __shared__ float top[kTreeNodes], maxima[kVerifyWaves], hit_logit[kVerifyWaves];
   __shared__ uint32_t places[kVerifyWaves], hit[kVerifyWaves], last[kVerifyWaves], zeros[kVerifyThreads];
-  __shared__ struct { int32_t code; uint32_t lack, place, child, subtracted; } told;   // by wavefront 0
+  __shared__ struct { int32_t code; uint32_t lack, place, child, subtracted; float most; } told;   // by wavefront 0 (most: what weights are against)
   __shared__ uint8_t path[kTreeNodes];
   __shared__ int32_t tokens[kTreeNodes];   // -1: none; wavefront 0 has them at once, the others behind the first round
   __shared__ float uniforms[kTreeNodes];
@@ -234,9 +239,25 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
   auto draft_of = [&](uint32_t node) { return a.draft + (size_t)(begin + node) * a.draft_stride; };
   auto parents_of = [&](uint32_t i) { return i == 0u ? tree.of[0] : i == 1u ? tree.of[1] : i == 2u ? tree.of[2] : tree.of[3]; };   // of the nodes 64 i + lane
 
+  // ---- tokens that were chosen and refused: of the node's children in front of the `from`-th, a thread each (-1: none)
+  auto refused = [&](uint32_t node, uint32_t from) {
+    return threadIdx.x < nodes && threadIdx.x < from && parents_of(wave) == (int32_t)node ? tokens[threadIdx.x] : -1;
+  };
+  // Which of a thread's elements of the step from v0 on are the token of another thread (or its own): a bit each, in `zeros` of the thread that load
+  // (of E elements) number n of the step belongs to, thread_of(n), from first_of(n) on.  By all threads.
+  auto mark = [&](int32_t gone, uint32_t v0, auto thread_of, auto first_of) {
+    zeros[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t n = ((uint32_t)gone - v0) / E;
+    if (gone >= 0 && (uint32_t)gone >= v0 && n < kVerifyStep / E) atomicOr(&zeros[thread_of(n)], 1u << (first_of(n) + (uint32_t)gone - row_start(v0 + n * E, a.vocab, E)));
+    __syncthreads();
+    return zeros[threadIdx.x];
+  };
+
   // ---- a chunk of a node's row, by the workgroup: a wavefront's largest logit, its first place, and the sum of the weights against that; then, in
-  // wavefront 0, the chunk's (in m a NaN: the row has no distribution).  The first step's logits may be there already.
-  auto sum_weights = [&](uint32_t node, uint32_t chunk, float (&ahead)[kVerifyLane], bool there, float& m, double& sum, uint32_t& first) {
+  // wavefront 0, the chunk's (in m a NaN: the row has no distribution).  The first step's logits may be there already.  less: without the
+  // tokens that are gone.
+  auto sum_weights = [&](uint32_t node, uint32_t chunk, float (&ahead)[kVerifyLane], bool there, bool less, int32_t gone, float& m, double& sum, uint32_t& first) {
     float most = -INFINITY;
     uint32_t at = 0xFFFFFFFFu;
     double s = 0.;
@@ -246,6 +267,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       float y[kVerifyLane];
 #pragma unroll
       for (uint32_t j = 0; j < kVerifyLane; ++j) y[j] = ahead[j];
+      if (!DRAFT && less) {
+        const uint32_t out = mark(gone, chunk * chunk_logits + step * kVerifyStep, [](uint32_t n) { return n % kVerifyThreads; }, [](uint32_t n) { return n / kVerifyThreads * E; });
+#pragma unroll
+        for (uint32_t j = 0; j < kVerifyLane; ++j) y[j] = out >> j & 1u ? -INFINITY : y[j];
+      }
       if (step + 1u < p.steps) request(node, chunk, step + 1u, ahead);   // (one step ahead / not: 16 x 64 nodes 33 to 41 / 36 to 43 us)
       float mx = y[0];
 #pragma unroll
@@ -342,29 +368,34 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     }
     return c;
   };
-  // Tokens that were chosen: r is w without the refused tokens, mass its sum; part are the sums of the lane's chunks, and lose them too.
-  // The first children are among the nodes that the node itself is among.
-  auto try_chosen = [&](uint32_t node, const Children& near, double m, uint32_t largest, double mass, double (&part)[kVerifyEach]) -> int32_t {
+  // Tokens that were chosen: r is w without the refused tokens, mass its sum; part are the sums of the lane's chunks, and lose them too.  The children
+  // from `child` on, until one is accepted or what is left is to be summed anew.  near: those among the nodes that `child` is among.
+  auto try_chosen = [&](uint32_t node, const Children& near, double m, uint32_t largest, uint32_t& child, double mass, double (&part)[kVerifyEach]) -> int32_t {
+    const double enough = mass * kVerifyLeft;
 #pragma unroll 1
-    for (uint32_t i = node >> 6; i * 64u < nodes; ++i) {
-      const Children c = i == node >> 6 ? near : children_of(node, i);
+    for (uint32_t i = child >> 6; i * 64u < nodes; ++i) {
+      const Children c = i == child >> 6 ? near : children_of(node, i);
       if (greedy) {
         const uint64_t same = __ballot(c.token >= 0 && (uint32_t)c.token == largest);
         if (same) return (int32_t)(64u * i + (uint32_t)__builtin_ctzll(same));
         continue;
       }
       const double w = c.token >= 0 ? weight(c.x, m, k) : 0.;
-      for (uint64_t set = __ballot(c.token >= 0); set; set &= set - 1ull) {
+      for (uint64_t set = __ballot(c.token >= 0 && 64u * i + lane >= child); set; set &= set - 1ull) {
         const uint32_t j = (uint32_t)__builtin_ctzll(set);
         const int32_t mine = __builtin_amdgcn_readlane(c.token, j);
         bool twin = lane < j && c.token == mine;   // of an earlier child: ruled out by now
         for (uint32_t g = node >> 6; g < i; ++g) twin |= parents_of(g) == (int32_t)node && 64u * g + lane < nodes && tokens[64u * g + lane] == mine;
         const double r = __any(twin) ? 0. : lane64(w, j), u = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c.u), j));
-        if (u * mass < r) return (int32_t)(64u * i + j);
-        if (mass - r > 0.) mass -= r;
+        if (u * mass < r || r >= mass) return (int32_t)(64u * i + j);   // (r is mass where no other token is left: u < 1)
+        mass -= r;
         const uint32_t of = (uint32_t)mine / chunk_logits;
 #pragma unroll
         for (uint32_t h = 0; h < kVerifyEach; ++h) part[h] = of == 64u * h + lane ? fmax(0., part[h] - r) : part[h];
+        if (mass < enough) {
+          child = 64u * i + j + 1u;
+          return kRefused;
+        }
       }
     }
     return kNone;
@@ -435,7 +466,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       double sum = 0.;
       uint32_t first = 0;
       if (DRAFT && rest) sum_rest(at, chunk, subtracted, y, sum);
-      else sum_weights(at, chunk, y, there && patience, m, sum, first);
+      else sum_weights(at, chunk, y, there && patience, rest, rest ? refused(at, child) : -1, m, sum, first);
       there = false;
       if (patience) {
         if (wave == 0) leave(m, sum, first);
@@ -480,7 +511,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
           // ---- the row's sums over its chunks, and the node's children
           int32_t c = kNoDistribution;
           double m;
-          if (!rest) {
+          if (!DRAFT || !rest) {
             float mc = part_max[0];
             bool none = part_max[0] != part_max[0];
 #pragma unroll
@@ -499,11 +530,15 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
             drawn = 0.;
             const uint32_t largest = greedy ? wave_min_u32(place) : 0u;
             if (lane == 0) {
-              top[at] = most;
-              total[at] = mass;
+              if (!rest) {
+                top[at] = most;
+                total[at] = mass;
+              }
+              told.most = most;
               told.place = largest;
             }
-            if (!__any(none) && most > -INFINITY) c = !DRAFT || greedy ? try_chosen(at, near, m, largest, mass, now) : kRefused;
+            if (!__any(none) && most > -INFINITY) c = !DRAFT || greedy ? try_chosen(at, near, m, largest, child, mass, now) : kRefused;
+            if (!DRAFT && lane == 0) told.child = child;
           } else {
             m = (double)top[at];
             double s = 0.;
@@ -536,11 +571,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     }
     // ---- the walk
     ended = (int32_t)uniform_u32((uint32_t)told.code);
-    if (DRAFT) {
-      child = uniform_u32(told.child);
-      subtracted = uniform_u32(told.subtracted);
-    }
-    rest = DRAFT && ended == kRefused;
+    rest = ended == kRefused;
+    if (DRAFT) subtracted = uniform_u32(told.subtracted);
+    if (DRAFT || rest) child = uniform_u32(told.child);
     if (rest) {
       ++subtracted;
       continue;
@@ -598,8 +631,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
     int32_t token = ended == kNone && greedy ? (int32_t)told.place : -1;
     float logit = 0.f;   // the token's
     if (draws) {
-      int32_t gone = -1;   // a child's token of the node: refused, as all of them are
-      if (!DRAFT && threadIdx.x < nodes && threadIdx.x > at && as_global(a.parents)[begin + threadIdx.x] == (int32_t)at) gone = tokens[threadIdx.x];
+      const int32_t gone = DRAFT ? -1 : refused(at, nodes);   // (all children have been refused)
       for (; chunk != kVerifyChunks; choose()) {
         if (lane == 0) { hit[wave] = 0xFFFFFFFFu; last[wave] = 0; }
         double front = 0.;
@@ -609,18 +641,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
           float z[kVerifyLane];
           load_row<kVerifyLane, E>(row_of(at), v, a.vocab, -INFINITY, y);
           if (DRAFT && subtracted) load_row<kVerifyLane, E>(draft_of(at), v, a.vocab, 0.f, z);
-          if (!DRAFT) {
-            zeros[threadIdx.x] = 0;
-            __syncthreads();
-            const uint32_t o = ((uint32_t)gone - v0) / E * E;   // its load
-            if (gone >= 0 && (uint32_t)gone >= v0 && o < kVerifyStep) atomicOr(&zeros[o / kVerifyLane], 1u << (o % kVerifyLane + (uint32_t)gone - row_start(v0 + o, a.vocab, E)));
-            __syncthreads();
-          }
-          const uint32_t zero = DRAFT ? 0u : zeros[threadIdx.x];
+          const uint32_t zero = DRAFT ? 0u : mark(gone, v0, [](uint32_t n) { return n / V; }, [](uint32_t n) { return n % V * E; });
           double r[kVerifyLane], s = 0.;
-          const double m = (double)top[at];
+          const double m = (double)told.most;
 #pragma unroll
-          for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = weight(y[j], m, k);
+          for (uint32_t j = 0; j < kVerifyLane; ++j) r[j] = weight(y[j], m, k);   // (of one that is gone it may be anything)
           if constexpr (DRAFT) {
             for (uint32_t i = 0; i < subtracted; ++i) {
               const double o = over[i], f = scale[i];

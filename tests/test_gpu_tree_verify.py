@@ -1,6 +1,7 @@
 """mpk_tree_verify on the GPU against the definition in 64 bits."""
 import math
 import random
+from fractions import Fraction
 
 import pytest
 import torch
@@ -440,3 +441,126 @@ def test_beside_work_that_fills_the_gpu(draft):
     for out in outs:
         assert all(torch.equal(p.view(torch.int32), r.view(torch.int32)) for p, r in zip(out, outs[0]))
     _check(m, begin, parents, tokens, x, outs[0], temps, uniforms, q, draft == "once")
+
+
+BELOW_ONE = 1 - 2 ** -24
+
+
+def _places(vocab, n):
+    """n tokens that lie in many chunks of a row: its first and last among them."""
+    return [0] if n == 1 else [i * (vocab - 1) // (n - 1) for i in range(n)]
+
+
+def _star(m, x, children, uniforms, temperature=1.0):
+    """Children of a root, against the definition.  Their own rows are flat: with V equal weights the first v with (v + 1) / V > u is floor(u V),
+    in whole numbers here (a sum of rounded shares may lie on either side where u V is whole)."""
+    V, nodes = x.shape[0], 1 + len(children)
+    logits = torch.zeros(nodes, V)
+    logits[0] = x
+    parents, tokens = [-1] + [0] * len(children), [0] + children
+    out = m.verify([0, nodes], parents, tokens, logits.cuda(), workspace(), temperatures=[temperature], uniforms=uniforms)
+    m.status()
+    walk, token, logs = verify_exact(parents, tokens, logits, temperature, uniforms)
+    if len(walk) == 2:
+        token = int(Fraction(float(torch.tensor(uniforms[0]))) * V)
+    rest = nodes - len(walk)
+    assert [int(out[0][0]), out[1].tolist(), int(out[2][0])] == [len(walk), walk + [-1] * rest, token]
+    want = torch.tensor(logs + [0.0] * rest, dtype=torch.float64)
+    assert ((out[3].cpu().double() - want).abs() <= F32_HALF * want.abs() + 2e-9).all()   # as in _check
+    return out
+
+
+@pytest.mark.parametrize("vocab", [0, 700, 5000, 150001])   # 0: the tokens alone
+@pytest.mark.parametrize("gaps,u", [
+    # a child that holds all but some 1e-7 of what is left is refused by the largest number below one; the last one is left alone
+    ([16.1], [BELOW_ONE, BELOW_ONE]), ([16.125, 16.125], [BELOW_ONE, BELOW_ONE, 0.5]), ([16.125, 16.125], [BELOW_ONE] * 3),
+    ([16.5] * 11, [BELOW_ONE] * 11 + [0.5]), ([16.5] * 11, [BELOW_ONE] * 12),
+    # large shares, refused by numbers of the ordinary size; then two alike
+    ([2.0, 3.0, 1.5, 4.0], [0.95, 0.97, 0.9, 0.99, BELOW_ONE]), ([16.5, 16.5, 0.0], [BELOW_ONE, BELOW_ONE, 0.75, BELOW_ONE])])
+def test_children_that_hold_all_there_is(gaps, u, vocab):
+    """Every token that is not ruled out is a child: the walk goes on at one of them, whatever the numbers."""
+    heights = [0.0]
+    for g in gaps:
+        heights.append(heights[-1] - g)
+    V = vocab or len(heights)
+    x, at = torch.full((V,), -math.inf), _places(V, len(heights))
+    x[at] = torch.tensor(heights)
+    out = _star(TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1), x, at, [0.5] + u)
+    assert int(out[0][0]) == 2 and int(out[2][0]) >= 0
+
+
+@pytest.mark.parametrize("root", [0.0, 0.3, 0.8, BELOW_ONE])
+@pytest.mark.parametrize("vocab", [40, 3000, 70001])
+@pytest.mark.parametrize("children,gap", [(1, 16.5), (2, 16.5), (7, 16.25), (3, 7.0), (1, 7.0)])
+def test_tokens_behind_children_that_hold_nearly_all(children, gap, vocab, root):
+    """Refused children leave tokens of much less probability than the row began with; one is drawn, in chunks of the children and others."""
+    gen = torch.Generator().manual_seed(children + vocab)
+    low = -gap * children
+    x, at = low + torch.randn(vocab, generator=gen) - math.log(vocab), _places(vocab, children)
+    x[at] = -gap * torch.arange(children, dtype=torch.float32)
+    out = _star(TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=vocab, layers=1), x, at, [root] + [BELOW_ONE] * children)
+    assert int(out[0][0]) == 1 and int(out[2][0]) not in at
+
+
+@pytest.mark.parametrize("last", [0.5, BELOW_ONE])
+@pytest.mark.parametrize("order", range(4))
+def test_children_in_many_groups_hold_all_there_is(order, last):
+    """As above with 255 children: unlikely ones, twins and out of turn, around a few that hold nearly all."""
+    V, rng = 9000, random.Random(order)
+    heavy = [rng.randrange(V) for _ in range(5)]
+    light = [t for t in rng.sample(range(V), 260) if t not in heavy][:100]
+    children = light + [rng.choice(light) for _ in range(255 - 5 - 20 - len(light))]
+    for h in heavy:   # in ascending order of their places, twins of them behind them
+        children.insert(rng.randrange(40) + 45 * heavy.index(h), h)
+    behind = max(children.index(h) for h in heavy)
+    for _ in range(20):
+        children.insert(rng.randint(behind + 1, len(children)), rng.choice(heavy[:4]))
+    x = torch.full((V,), -math.inf)
+    x[light] = -120.0 - torch.rand(len(light), generator=torch.Generator().manual_seed(order))
+    turn = sorted(heavy, key=children.index)
+    x[turn] = -16.5 * torch.arange(5, dtype=torch.float32)
+    u = [0.5] + [BELOW_ONE if c in heavy else 0.6 for c in children]
+    u[1 + children.index(turn[-1])] = last
+    out = _star(TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1), x, children, u)
+    assert out[1].tolist()[1] == 1 + children.index(turn[-1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("temperatures", [[1.0], [0.5, 1.0, 0.0, 2.0]])
+def test_walks_through_nodes_whose_children_hold_nearly_all(temperatures, dtype):
+    """Several sequences, late workgroups: at each node a few tokens in steps of some 16 temperatures, the likeliest first among the children,
+    numbers that refuse most of them."""
+    V, lens, gen = 30011, [12, 1, 40, 9, 25], torch.Generator().manual_seed(2)
+    m = TreeModel(n_q=2, n_kv=1, batch=8, max_seq=8, vocab=V, layers=1, debug_flags=M.DEBUG_JITTER)
+    begin, parents = _begin(lens), sum((tree(n, "random", 50 + i) for i, n in enumerate(lens)), [])
+    x = torch.full((begin[-1], V), -math.inf)
+    tokens, uniforms, temps = [0] * begin[-1], [0.37] * begin[-1], [temperatures[i % len(temperatures)] for i in range(len(lens))]
+    for i in range(len(lens)):
+        kids = {}
+        for t in range(begin[i], begin[i + 1]):
+            row = torch.randperm(V, generator=gen)
+            step = 16.5 * (temps[i] or 1.0)
+            x[t, row[:6]] = -step * torch.arange(6, dtype=torch.float32)
+            x[t, row[6:400]] = -6 * step + torch.randn(394, generator=gen) - 8.0
+            p = parents[t]
+            if p >= 0:
+                j = kids[p] = kids.get(p, -1) + 1
+                order = x[begin[i] + p].sort(descending=True).indices
+                tokens[t] = int(order[min(j, 5)])
+                uniforms[t] = BELOW_ONE if (t + j) % 3 else 0.61
+    logits = x.to(dtype)
+    for _ in range(3):
+        out = m.verify(begin, parents, tokens, logits.cuda(), workspace(), temperatures=temps, uniforms=uniforms)
+        m.status()
+        _check(m, begin, parents, tokens, logits, out, temps, torch.tensor(uniforms), None)
+
+
+def test_equal_shares_are_exact():
+    """Of eight equal tokens four are refused: u = 1/4 refuses the fifth (u q < r is strict), the number in front of it accepts."""
+    m = TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=8, layers=1)
+    for u, length in ((0.25, 1), (0.25 - 2 ** -26, 2)):
+        out = m.verify([0, 6], [-1, 0, 0, 0, 0, 0], [0, 7, 1, 4, 2, 3], torch.full((6, 8), 3.25).cuda(), workspace(), temperatures=[1.3],
+                       uniforms=[0.0] + [BELOW_ONE] * 4 + [u])
+        m.status()
+        assert int(out[0][0]) == length
+        assert length == 2 or int(out[2][0]) == 0
