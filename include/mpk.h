@@ -705,7 +705,7 @@ mpk_status mpk_tree_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  *   logprobs     : device fp32 [n_rows] or NULL: in the place of a path's node, ln p of the token behind that node (the path's next, or
  *                  next_tokens); 0 in the sequence's others.  (temperature 0: p is of the logits as they are)
  *   workspace    : device, MPK_ROWS_WORKSPACE_BYTES: the call may use it (sums go through memory of the graph's today)
- * Results do not overlap each other or what the call reads.
+ * Results do not overlap each other or what the call reads (refused among results and lists; of logits and draft_probs where a result holds their beginning).
  * p, r, sums and comparisons are in 64 bits.  A logit of -inf is a token ruled out.  At a node whose row holds a NaN or +inf, or nothing
  * above -inf, the walk ends: next_tokens is -1, its logprob NaN.
  * Device errors: row_begin not ascending or outside 0 .. n_rows (lengths 0, next_tokens -1, nothing else is written); more nodes than
@@ -721,7 +721,7 @@ mpk_status mpk_tree_verify(mpk_graph *g, uint32_t n_seqs, uint32_t n_rows, const
 /* The cache rows of an accepted path close up, K and V of every layer: row positions[i] + path[row_begin[i] + k] moves to
  * positions[i] + k, for k below lengths[i].  (A node of the path at place k of it has depth k: its row has the angle of where it then is.)
  *   n_seqs .. positions : as above;  lengths, path : as mpk_tree_verify leaves them
- *   positions_out : device int32 [n_seqs] or NULL: positions[i] + lengths[i], what the next step starts from; none of the other lists
+ *   positions_out : device int32 [n_seqs] or NULL: positions[i] + lengths[i], what the next step starts from; apart from the other lists
  * Device errors as mpk_tree_append; also a length outside 0 .. the tree's nodes, a path that does not ascend within
  * it (the sequence is left out, its position stays), a page outside the pool (its rows are left out). */
 mpk_status mpk_tree_keep(mpk_graph *g, uint32_t n_seqs, uint32_t n_rows, const int32_t *row_begin,

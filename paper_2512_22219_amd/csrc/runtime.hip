@@ -1159,14 +1159,26 @@ static mpk_status rows_words(const char* name, const void* p) {   // (NULL where
   if ((uintptr_t)p % 4) { set_error("%s is not aligned to its elements", name); return MPK_ERR_INVALID_ARG; }
   return MPK_OK;
 }
-// Results where workgroups that are not through still read.
-static mpk_status rows_apart(std::initializer_list<std::pair<const char*, const void*>> results, std::initializer_list<std::pair<const char*, const void*>> lists) {
+// Results where workgroups that are not through still read, or on each other.
+struct RowsSpan {
+  const char* name;
+  const void* at;   // NULL: not given, or not looked at
+  size_t bytes;
+};
+static mpk_status rows_apart(std::initializer_list<RowsSpan> results, std::initializer_list<RowsSpan> lists) {
+  auto meet = [](const RowsSpan& x, const RowsSpan& y) {
+    const uintptr_t p = (uintptr_t)x.at, q = (uintptr_t)y.at;
+    return p && q && x.bytes && y.bytes && (p < q ? q - p < x.bytes : p - q < y.bytes);
+  };
+  auto refuse = [](const RowsSpan& x, const RowsSpan& y) {
+    set_error("%s %s %s", x.name, x.at == y.at ? "is" : "overlaps", y.name);
+    return MPK_ERR_INVALID_ARG;
+  };
   for (auto r = results.begin(); r != results.end(); ++r) {
-    if (!r->second) continue;
     for (const auto& l : lists)
-      if (l.second == r->second) { set_error("%s is %s", r->first, l.first); return MPK_ERR_INVALID_ARG; }
+      if (meet(*r, l)) return refuse(*r, l);
     for (auto o = results.begin(); o != r; ++o)
-      if (o->second == r->second) { set_error("%s is %s", r->first, o->first); return MPK_ERR_INVALID_ARG; }
+      if (meet(*r, *o)) return refuse(*r, *o);
   }
   return MPK_OK;
 }
@@ -1348,10 +1360,12 @@ extern "C" mpk_status mpk_tree_verify(mpk_graph* g, uint32_t n_seqs, uint32_t n_
     if (row_stride < vocab) { set_error("a row stride of %zu elements, the vocabulary has %u", row_stride, vocab); return MPK_ERR_INVALID_ARG; }
     if (draft_probs && draft_stride < vocab) { set_error("draft_probs: a row stride of %zu elements, the vocabulary has %u", draft_stride, vocab); return MPK_ERR_INVALID_ARG; }
     if ((st = rows_work(workspace)) != MPK_OK) return st;
-    if ((st = rows_apart({{"lengths", lengths}, {"path", path}, {"next_tokens", next_tokens}, {"logprobs", logprobs}},
-                         {{"row_begin", row_begin}, {"parents", parents}, {"tokens", tokens}, {"logits", logits}, {"draft_probs", draft_probs},
-                          {"temperatures", temperatures}, {"uniforms", uniforms}})) != MPK_OK) return st;
   }
+  const size_t seqs = 4 * (size_t)n_seqs, rows = 4 * (size_t)n_rows;   // (of logits and draft_probs by where they begin: which rows are read is seen on the device)
+  if ((st = rows_apart({{"lengths", lengths, seqs}, {"path", path, rows}, {"next_tokens", next_tokens, seqs}, {"logprobs", logprobs, rows}},
+                       {{"row_begin", row_begin, seqs + 4}, {"parents", parents, rows}, {"tokens", tokens, rows}, {"logits", logits, n_rows ? 1u : 0u},
+                        {"draft_probs", draft_probs, n_rows ? 1u : 0u}, {"temperatures", temperatures, seqs},
+                        {"uniforms", temperatures ? uniforms : nullptr, rows}})) != MPK_OK) return st;
   if ((st = rows_runnable(g)) != MPK_OK) return st;
   VerifyArgs a{};
   a.row_begin = row_begin; a.parents = parents; a.tokens = tokens;
@@ -1372,7 +1386,9 @@ extern "C" mpk_status mpk_tree_keep(mpk_graph* g, uint32_t n_seqs, uint32_t n_ro
   if (st != MPK_OK) return st;
   if (n_rows && (!lengths || !path)) { set_error("NULL argument"); return MPK_ERR_INVALID_ARG; }
   if ((st = rows_words("lengths", lengths)) != MPK_OK || (st = rows_words("path", path)) != MPK_OK || (st = rows_words("positions_out", positions_out)) != MPK_OK) return st;
-  if ((st = rows_apart({{"positions_out", positions_out}}, {{"row_begin", row_begin}, {"slots", slots}, {"positions", positions}, {"lengths", lengths}, {"path", path}})) != MPK_OK) return st;
+  const size_t seqs = 4 * (size_t)n_seqs;
+  if ((st = rows_apart({{"positions_out", positions_out, seqs}}, {{"row_begin", row_begin, seqs + 4}, {"slots", slots, seqs}, {"positions", positions, seqs},
+                       {"lengths", n_rows ? lengths : nullptr, seqs}, {"path", path, 4 * (size_t)n_rows}})) != MPK_OK) return st;
   if ((st = rows_cache_runnable(g)) != MPK_OK) return st;
   a.n_layers = g->h.cfg.n_layers;
   a.layer_stride = rows_of_layer(g->h) * a.s.n_kv * a.s.head_dim;

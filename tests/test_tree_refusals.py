@@ -133,3 +133,45 @@ def test_constants():
     text = open(M.binding.__file__.replace("paper_2512_22219_amd/binding.py", "include/mpk.h")).read()
     assert "#define MPK_TREE_MAX_NODES 256u" in text and M.TREE_MAX_NODES == 256
     assert "#define MPK_TREE_DRAWN_ONCE 1u" in text and M.TREE_DRAWN_ONCE == 1
+
+
+def test_results_of_no_rows_on_what_is_read(model):
+    """Lengths and next tokens are written for calls of no rows too."""
+    far = dict(VERIFY, n_rows=0, **{n: P + 4096 * (i + 9) for i, n in enumerate(("begin", "temperatures", "uniforms", "lengths", "next"))})
+    _refused(model.graph.tree_verify, *far.values(), match="host_only")
+    _refused(model.graph.tree_verify, *dict(far, next=far["lengths"]).values(), match="next_tokens is lengths")
+    for name, says in (("lengths", "lengths"), ("next", "next_tokens")):
+        _refused(model.graph.tree_verify, *dict(far, **{name: far["begin"]}).values(), match=f"{says} is row_begin")
+        _refused(model.graph.tree_verify, *dict(far, **{name: far["temperatures"]}).values(), match=f"{says} is temperatures")
+        _refused(model.graph.tree_verify, *dict(far, **{name: far["uniforms"]}).values(), match="host_only")   # (not looked at)
+    _refused(model.graph.tree_verify, *dict(far, path=far["lengths"], logprobs=far["lengths"]).values(), match="host_only")
+
+
+@pytest.mark.parametrize("rows", [0, 7])
+@pytest.mark.parametrize("result", ["lengths", "path", "next", "logprobs"])
+def test_results_that_begin_or_end_inside_a_list(model, result, rows):
+    says = dict(begin="row_begin", next="next_tokens")
+    count = dict(begin=4, parents=rows, tokens=rows, temperatures=3, uniforms=rows, lengths=3, path=rows, next=3, logprobs=rows)
+    far = dict(VERIFY, n_seqs=3, n_rows=rows, **{n: P + 65536 * (i + 1) for i, n in enumerate(VERIFY) if VERIFY[n] >= P})
+    for on, n in count.items():
+        if on == result:
+            continue
+        name, other = says.get(result, result), says.get(on, on)
+        both = f"({name} overlaps {other}|{other} overlaps {name})" if n and count[result] else "host_only"
+        for off in (4, 4 * (n - 1), -4, -4 * (count[result] - 1)):
+            if off:
+                _refused(model.graph.tree_verify, *dict(far, **{result: far[on] + off}).values(), match=both)
+        for off in (4 * n, -4 * count[result]):   # side by side
+            if off:
+                _refused(model.graph.tree_verify, *dict(far, **{result: far[on] + off}).values(), match="host_only")
+
+
+def test_new_positions_that_begin_or_end_inside_a_list(model):
+    says = dict(begin="row_begin")
+    far = dict(KEEP, n_seqs=3, n_rows=7, slots=P, **{n: P + 65536 * (i + 1) for i, n in enumerate(KEEP) if KEEP[n] >= P})
+    far["slots"] = P + 65536 * 20
+    for on, n in dict(begin=4, slots=3, positions=3, lengths=3, path=7).items():
+        for off in (4, 4 * (n - 1), -4, -8):
+            _refused(model.graph.tree_keep, *dict(far, out=far[on] + off).values(), match=f"positions_out overlaps {says.get(on, on)}")
+        for off in (4 * n, -12):
+            _refused(model.graph.tree_keep, *dict(far, out=far[on] + off).values(), match="host_only")
