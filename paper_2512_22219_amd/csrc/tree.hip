@@ -34,8 +34,10 @@ constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
 constexpr uint32_t kVerifyLane = 8, kVerifyStep = kVerifyThreads * kVerifyLane;
 constexpr uint32_t kVerifyEach = kVerifyChunks / 64;   // chunks of a lane when they are joined: the lane-th, the 64 + lane-th
 constexpr uint32_t kVerifyWorkgroups = 768;   // of a call at most: as many as run at once, three a compute unit
-// Ticks of 10 ns until others' sums are worked out: several rounds, so that it happens only where a workgroup does not run.
-constexpr uint32_t kVerifyPatience = 2000;
+// Ticks of 10 ns until others' sums are worked out: several rounds, and more by the steps of a chunk and the subtractions in them, so that it happens
+// only where a workgroup does not run.  (16 rows of 4 million logits, 43 steps, in bf16 and drawn, 412 us, with 20 us whatever the steps 654; 8 million
+// in fp32, sampled, 271, 323.)
+constexpr uint32_t kVerifyPatience = 2000, kVerifyPatienceStep = 200, kVerifyPatienceLess = 20;
 // Refused chosen tokens are taken off the sums until less than this is left of them; then what is left is summed anew, against its own largest logit.
 // A difference has the sums' error, some 1e-13 of what they began with, so what is compared with random numbers and drawn from stays within 1e-10.  A
 // node comes to this with the same probability: its numbers have refused all the rest.
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
       part[h] = 0.;
       part_place[h] = 0xFFFFFFFFu;
     }
-    for (uint32_t patience = kVerifyPatience;; patience = 0) {
+    for (uint32_t patience = kVerifyPatience + (p.steps - 1u) * kVerifyPatienceStep + (DRAFT && rest ? p.steps * subtracted * kVerifyPatienceLess : 0u);; patience = 0) {
       float m = 0.f;
       double sum = 0.;
       uint32_t first = 0;

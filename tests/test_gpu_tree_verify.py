@@ -564,3 +564,10 @@ def test_equal_shares_are_exact():
         m.status()
         assert int(out[0][0]) == length
         assert length == 2 or int(out[2][0]) == 0
+
+
+@pytest.mark.parametrize("draft", [None, "drawn"])
+def test_verify_rows_of_many_steps_a_workgroup(draft):
+    """Sixteen rows of 1.2 million logits, 13 steps of a workgroup each: chunks that take longer than others wait by default."""
+    lens = [2, 1, 1, 3, 1, 1, 2, 1, 1, 1, 2, 1, 1, 1, 1, 1]
+    _case(12, 1200000, lens, ["chain"] * 16, torch.bfloat16, draft, [1.0, 0.8, 0.0], std=3.0)
