@@ -391,9 +391,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
         const double r = __any(twin) ? 0. : lane64(w, j), u = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c.u), j));
         if (u * mass < r || r >= mass) return (int32_t)(64u * i + j);   // (r is mass where no other token is left: u < 1)
         mass -= r;
-        const uint32_t of = (uint32_t)mine / chunk_logits;
+        const uint32_t of = (uint32_t)mine / chunk_logits;   // (something: what is left of a chunk may be lost in the difference, and u = 0 draws it)
 #pragma unroll
-        for (uint32_t h = 0; h < kVerifyEach; ++h) part[h] = of == 64u * h + lane ? fmax(0., part[h] - r) : part[h];
+        for (uint32_t h = 0; h < kVerifyEach; ++h) part[h] = of == 64u * h + lane ? fmax(0x1p-1000, part[h] - r) : part[h];
         if (mass < enough) {
           child = 64u * i + j + 1u;
           return kRefused;
@@ -702,7 +702,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) tree_verify_kernel(VerifyAr
         }
         if (token < 0) token = (int32_t)late - 1;
         if (token >= 0) break;
-        if (threadIdx.x == 0) part_sum[chunk] = 0.;   // (a sum that was rounding alone)
+        if (threadIdx.x == 0) part_sum[chunk] = 0.;   // (nothing was left of it)
         __syncthreads();
       }
     }

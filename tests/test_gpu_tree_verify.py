@@ -571,3 +571,19 @@ def test_verify_rows_of_many_steps_a_workgroup(draft):
     """Sixteen rows of 1.2 million logits, 13 steps of a workgroup each: chunks that take longer than others wait by default."""
     lens = [2, 1, 1, 3, 1, 1, 2, 1, 1, 1, 2, 1, 1, 1, 1, 1]
     _case(12, 1200000, lens, ["chain"] * 16, torch.bfloat16, draft, [1.0, 0.8, 0.0], std=3.0)
+
+
+@pytest.mark.parametrize("root", [0.0, 2 ** -24, 0.4, BELOW_ONE])
+@pytest.mark.parametrize("low", [-40.0, -90.0, -math.inf])
+@pytest.mark.parametrize("heavy", [[1055, 3388], [3388, 1055], [0, 2047, 4999], [2100, 2101, 2102, 4100], [4999, 0, 4998]])
+def test_a_chunk_that_its_refused_tokens_leave_hardly_anything_of(heavy, low, root):
+    """All but the last of the likely tokens are refused, by ordinary numbers: u = 0 draws the first token that has any probability, of a chunk
+    whose sum does not show it too."""
+    V, gen = 5000, torch.Generator().manual_seed(len(heavy))
+    x = low + torch.randn(V, generator=gen) if low > -math.inf else torch.full((V,), low)
+    x[heavy] = 0.7 + 0.01 * torch.arange(len(heavy)).float()
+    out = _star(TreeModel(n_q=2, n_kv=1, batch=4, max_seq=8, vocab=V, layers=1), x, heavy[:-1], [root] + [0.75] * (len(heavy) - 1))
+    assert int(out[0][0]) == 1
+    if root == 0.0:
+        first = 1 if 0 in heavy[:-1] else 0
+        assert int(out[2][0]) == (first if low > -math.inf else heavy[-1])
