@@ -648,7 +648,8 @@ mpk_status mpk_rows_logprobs(mpk_graph *g, uint32_t n_rows, const void *logits, 
  * alone).  The row at place t of its sequence, counted from 0, is node t; parents[row] is the place of its parent, below t, or -1.
  * With `positions[i]` rows of the sequence cached, node t is cached at row positions[i] + t, stands at position
  * positions[i] + depth(t), depth being the number of its ancestors, and sees the rows cached before, its
- * ancestors and itself.  A chain is what mpk_rows_append and mpk_rows_attend would make of the same rows.
+ * ancestors and itself.  Of a chain mpk_tree_append makes the same bits as mpk_rows_append of the same rows; mpk_tree_attend
+ * adds up keys in another order than mpk_rows_attend: the same to rounding.
  *
  * Common to the four: what is common to the calls on rows above, their workspace and errors included.  The cache rows behind the
  * accepted ones hold rejected nodes afterwards; nothing reads them before they are written again.
@@ -706,6 +707,8 @@ mpk_status mpk_tree_attend(mpk_graph *g, uint32_t layer, uint32_t n_seqs, uint32
  *                  next_tokens); 0 in the sequence's others.  (temperature 0: p is of the logits as they are)
  *   workspace    : device, MPK_ROWS_WORKSPACE_BYTES: the call may use it (sums go through memory of the graph's today)
  * Results do not overlap each other or what the call reads (refused among results and lists; of logits and draft_probs where a result holds their beginning).
+ * A sequence's workgroups exchange sums while they run.  Where the device has no room for all of a call's (other work beside it, fewer
+ * compute units), each waits some 20 us for what is missing and then works it out itself: the same results, several times as late.
  * p, r, sums and comparisons are in 64 bits.  A logit of -inf is a token ruled out.  At a node whose row holds a NaN or +inf, or nothing
  * above -inf, the walk ends: next_tokens is -1, its logprob NaN.
  * Device errors: row_begin not ascending or outside 0 .. n_rows (lengths 0, next_tokens -1, nothing else is written); more nodes than

@@ -10,24 +10,33 @@ namespace mpk {
 // The walk needs, of each node that it comes to, the largest logit m and Z = sum 2^(k (x - m)), k = log2(e) / temperature, in 64 bits: a random
 // number is compared with sums of up to a vocabulary of weights, and which side it falls on is a token.
 // It goes in rounds.  A round is a node of the walk or what is left of the node's distribution behind refused children: with a draft
-// distribution behind each; of chosen tokens, whose weights are taken off the row's sum meanwhile, where hardly anything is left (kVerifyLeft).  A row is cut into chunks, one for each of the sequence's workgroups.  Each leaves its sums where all of them read
-// them, reads all of them, and works out for itself how the walk goes on.
+// distribution behind each; of chosen tokens, whose weights are taken off the row's sum meanwhile, where hardly anything is left
+// (kVerifyLeft).  A row is cut into chunks, one for each of the sequence's workgroups.  Each leaves its sums where all of them read them,
+// reads all of them, and works out for itself how the walk goes on.
 // So a round is one pass over a chunk and one exchange between the compute units, and nobody waits for a decision to be passed on.
 // Nor does anybody depend on workgroups that may not run yet: sums that have not come after a while are worked out by
-// who needs them (the same operations in the same order, the same bits), so that each workgroup alone comes to the end.
+// who needs them (the same operations in the same order, the same bits), so that each workgroup alone comes to the end.  It takes its
+// time: beside products that fill the device a call waits for room, 64 nodes 280 to 520 us.
 //
-// Bound by the latency of the rounds, one behind the other; a row of 150000 logits is read in a fraction of a microsecond.  A round of one sequence
-// takes 4.4 us: the chunk's logits 0.6 to 0.9, weights 0.5, sums over the workgroup 0.5, the exchange 1.4 to 1.8, the row's sums and the children 1;
-// beside the rounds 2 us at the start (lists, the root's row) and 3 to 4 where a token is drawn.  A chain of 6, greedy, 8 to 17 us by what
-// is accepted, 64 nodes 14 to 19, 8 x 25 drawn nodes over 128256 logits in bf16 31 to 48, 16 x 64 33 to 41.
-// A workgroup a sequence takes 81, 505, 650 and 653 us for these.  No better were: units handed out by a counter, whoever comes last deciding
-// (atomics on one address take 20 ns each: 64 nodes 30 us); several nodes of the tree in a round (1 / 2 / 3: 64 nodes 20.8 / 20.6 / 20.8, 8 x 25 drawn
-// 48 / 59 / 68, a chain of 6 8.5 to 17.4 / 10.4 to 17.3 / 11.6); the chunk of the child that is tried next requested while the others' sums come (no
-// change: the wait is for the slowest of all), or summed as well (16.7 / 16.8, 18.2 / 19.7, 34.8 / 37.3, 40.5 / 43.4), or that by four wavefronts while a
-// fifth leads (a round 4.3 / 3.5 where that child is accepted, but 0.5 more once: a chain of 6 8.1 to 16.7 / 8.5 to 15.6, 64 nodes 18.2 / 19.2, 8 x 25 35.5 / 37.4;
-// and two workgroups a compute unit instead of three); what is left of a chunk kept in LDS from one refused child to the next (no change; 13 trees of 55 nodes,
-// ten children a node, 48.4 / 42.1); a sequence's workgroups on one XCD (one over 150000 logits 16.7 / 21.0, 13 over 19000 58.3 / 55.3; where it
-// is no more than one a compute unit 0.6 % of 52 calls' mean).
+// Bound by the latency of the rounds, one behind the other; a row of 150000 logits is read in a fraction of a microsecond.  A round of one
+// sequence takes 4.4 us: the chunk's logits 0.6 to 0.9, weights 0.5, sums over the workgroup 0.5, the exchange 1.4 to 1.8, the row's sums
+// and the children 1; beside the rounds 2 us at the start (lists, the root's row) and 3 to 4 where a token is drawn.  A chain of 6 takes,
+// greedy, 8.4 / 12.6 / 17.1 / 21.3 / 25.7 / 29.9 us with 0 / 1 / 2 / 3 / 4 / 5 tokens accepted, sampled 10.3 to 29.0.  Sampled, with one or two
+// accepted, 64 nodes 15 to 19; with three or four in the longest walk, 8 x 25 drawn nodes over 128256 logits in bf16 35 to 49, 16 x 64 33 to 40.
+// A workgroup a sequence took 505, 650 and 653 us for the last three, 81 for a chain.
+// No better were (as it is / so):
+//   - units handed out by a counter, whoever comes last deciding (atomics on one address take 20 ns each): 64 nodes 21 / 30
+//   - two or three nodes of the tree in a round (1 / 2 / 3): 64 nodes 20.8 / 20.6 / 20.8, 8 x 25 drawn 48 / 59 / 68, a chain of 6, up to two
+//     accepted, 8.5 to 17.4 / 10.4 to 17.3 / 11.6
+//   - the chunk of the child that is tried next requested while the others' sums come: no change, the slowest of all decides; or summed as
+//     well: a chain 16.7 / 16.8, 64 nodes 18.2 / 19.7, 8 x 25 34.8 / 37.3, 16 x 64 40.5 / 43.4
+//   - that by four wavefronts while a fifth leads: a round 4.3 / 3.5 where that child is accepted, but 0.5 more once and two workgroups a
+//     compute unit instead of three: a chain 8.1 to 16.7 / 8.5 to 15.6, 64 nodes 18.2 / 19.2, 8 x 25 35.5 / 37.4
+//   - what is left of a chunk kept in LDS from one refused child to the next: no change, but 48.4 / 42.1 for 13 trees of 55 nodes with ten
+//     children a node; 2 % more in the mean of 64 calls
+//   - a sequence's workgroups on one XCD: one over 150000 logits 16.7 / 21.0, 13 over 19000 58.3 / 55.3; by a rule on chunks an XCD 0.6 % less in
+//     52 calls' mean
+//   - words read by 16 bytes: no change
 constexpr uint32_t kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
 // Logits of a thread and of a workgroup at once.  Chunks of 2048 / 4096: 64 nodes 18.2 / 21.7 us, 8 x 25 drawn
 // 35.5 / 38.3.
